@@ -329,6 +329,117 @@ moe_status moe_forward_profiled(const moe_args* a, void* ws, size_t ws_bytes,
 #define MOE_STATIC_WS_BYTES (256u << 20)
 moe_status moe_forward_static_ws(const moe_args* a, hipStream_t stream);
 
+/*
+ * The dense half of a layer, with its backward passes: the norm in front of the
+ * router or of a feed-forward block, and the gated feed-forward block (a shared
+ * expert beside the routed ones, or the dense layers of a model).  As for every
+ * entry point, arrays are dense and row-major, device pointers 16-byte aligned,
+ * and nothing is allocated, synchronised or copied to the host.  Every sum and
+ * statistic is held in fp32, in a fixed order: results are the same on every
+ * run.  Infinities and NaN of a row stay in what that row feeds: its own outputs
+ * and the weights' gradients.
+ */
+typedef enum { MOE_DT_F32 = 0, MOE_DT_BF16 = 1, MOE_DT_F16 = 2 } moe_dtype;
+
+typedef enum {
+  MOE_NORM_LAYER = 0, /* about the mean of the row          */
+  MOE_NORM_RMS = 1    /* root mean square, no mean, no bias */
+} moe_norm_kind;
+
+/* Limits checked on the host. */
+#define MOE_MAX_WIDTH 65536
+#define MOE_MAX_ROWS (1 << 24)
+
+/*
+ * Norm of the rows of x [T,H], optionally of x + residual:
+ *   s = x + residual, rounded to the type and written to sum (x itself without)
+ *   xhat = (s - mean) * rstd, rstd = 1 / sqrt(mean((s - mean)^2) + eps); rms: mean = 0
+ *   y = xhat * weight + bias
+ *   x, residual, y, sum  device, dtype [T,H]; residual NULL for none (sum is then
+ *           not written and may be NULL)
+ *   weight, bias         device, dtype [H]; bias NULL for none (rms: must be)
+ *   mean, rstd           device, fp32 [T], for the backward pass; each may be NULL
+ *   0 <= T <= MOE_MAX_ROWS, 1 <= H <= MOE_MAX_WIDTH (any: rows need no alignment of
+ *   their own), eps >= 0 and finite.  T == 0 is a no-op.
+ * y or sum may be x or residual itself (each row is read before it is written),
+ * but not both the same array; no other overlap.
+ * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (kind, dtype, eps, a bias with rms),
+ * MOE_ERR_NULL, MOE_ERR_ALIGN, MOE_ERR_HIP.
+ */
+moe_status moe_norm_forward(const void* x, const void* residual, const void* weight, const void* bias, int T, int H,
+                            int kind, int dtype, float eps, void* y, void* sum, float* mean, float* rstd,
+                            hipStream_t stream);
+
+/* Workspace of moe_norm_backward where dweight or dbias is asked for; 0 for sizes
+ * it refuses. */
+size_t moe_norm_backward_workspace_bytes(int T, int H);
+
+/*
+ * Backward pass of moe_norm_forward: with g = dy * weight and means over a row,
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)) + dsum   (rms: no mean(g))
+ *   dweight[h] = sum_t dy * xhat,   dbias[h] = sum_t dy
+ *   dy, x       device, dtype [T,H]; x is what was normalised (sum, with a residual)
+ *   weight      device, dtype [H]
+ *   mean, rstd  device, fp32 [T], as the forward pass wrote them (mean may be NULL for rms)
+ *   dsum        device, dtype [T,H] or NULL: the gradient that reaches sum on its
+ *               other way; dx is then the gradient of x and of residual alike
+ *   dx          device, dtype [T,H]; may be dy or dsum itself, no other overlap
+ *   dweight, dbias  device, fp32 [H]; each may be NULL.  T == 0 writes zeros.
+ *   ws          moe_norm_backward_workspace_bytes(T, H) bytes, unused (may be NULL)
+ *               without dweight and dbias
+ * Errors: as moe_norm_forward (a dbias with rms: MOE_ERR_UNSUPPORTED), MOE_ERR_WORKSPACE.
+ */
+moe_status moe_norm_backward(const void* dy, const void* x, const void* weight, const float* mean, const float* rstd,
+                             const void* dsum, int T, int H, int kind, int dtype, void* dx, float* dweight,
+                             float* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Activation of the gate projection. */
+typedef enum {
+  MOE_ACT_SILU = 0,     /* g / (1 + exp(-g))                                          */
+  MOE_ACT_GELU_TANH = 1 /* g / 2 * (1 + tanh(sqrt(2/pi) * (g + 0.044715 * g^3)))      */
+} moe_act;
+
+/*
+ * The gated feed-forward block.  w1 and w2 are stored as one expert of the layer:
+ * the gate projection's I rows, then the up projection's.
+ *   pre = x w1^T (fp32);  h = act(pre[:, :I]) * pre[:, I:], rounded to dtype
+ *   y = h w2^T + add
+ * and backward, from dy and the saved pre,
+ *   dh = dy w2;  dpre = [dh * up * act'(gate), dh * act(gate)], rounded to dtype
+ *   dx = dpre w1;  dw1 = dpre^T x;  dw2 = dy^T h
+ * dtype is MOE_DT_BF16 or MOE_DT_F16 (fp16: an h or dpre past 65504 is an
+ * infinity, and small gradients want a scaled loss, as everywhere in fp16).
+ */
+typedef struct {
+  int32_t T;     /* rows, 0 .. MOE_MAX_ROWS                                */
+  int32_t H, I;  /* multiples of 8, at most MOE_MAX_WIDTH                  */
+  int32_t dtype; /* moe_dtype                                              */
+  int32_t act;   /* moe_act                                                */
+  const void* x;   /* [T,H]                                                */
+  const void* w1;  /* [2I,H]                                               */
+  const void* w2;  /* [H,I]                                                */
+  const void* add; /* forward: [T,H] or NULL; may be y itself              */
+  void* y;         /* forward: [T,H]                                       */
+  float* pre;      /* fp32 [T,2I]: forward writes it (NULL: not kept), backward reads it */
+  const void* dy;  /* backward: [T,H]                                      */
+  void* dx;        /* backward: [T,H], [2I,H], [H,I]; each may be NULL:    */
+  void* dw1;       /*   that gradient is then not computed                 */
+  void* dw2;
+} moe_ffn_args;
+
+/* Workspace of the forward and of the backward pass, from T, H, I; 0 for sizes
+ * they refuse. */
+size_t moe_ffn_workspace_bytes(const moe_ffn_args* a);
+size_t moe_ffn_backward_workspace_bytes(const moe_ffn_args* a);
+
+/*
+ * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (dtype, act), MOE_ERR_NULL,
+ * MOE_ERR_ALIGN, MOE_ERR_WORKSPACE, MOE_ERR_HIP.  T == 0 is a no-op forward; backward
+ * it writes zero weight gradients.
+ */
+moe_status moe_ffn_forward(const moe_ffn_args* a, void* ws, size_t ws_bytes, hipStream_t stream);
+moe_status moe_ffn_backward(const moe_ffn_args* a, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Static, NUL-terminated name of a status code. */
 const char* moe_status_str(int status);
 

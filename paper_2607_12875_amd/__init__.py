@@ -11,6 +11,8 @@ from ._binding import (  # noqa: F401
     STATIC_WS_BYTES, moe_forward_args, moe_forward_profiled, moe_forward_static_ws, moe_gate_topk, moe_permute, moe_permute_capacity,
     moe_router_gate_topk,
     moe_permute_workspace_bytes, moe_workspace_bytes, moe_workspace_layout,
+    MoeFfnArgs, make_ffn_args, moe_ffn_backward, moe_ffn_backward_workspace_bytes, moe_ffn_forward, moe_ffn_workspace_bytes,
+    moe_norm_backward, moe_norm_backward_workspace_bytes, moe_norm_forward,
     moe_peak_copy, moe_peak_mfma, moe_peak_mfma_flops_per_launch, moe_peak_read, moe_peak_sink_elems,
     moe_peak_lds_copy, moe_peak_lds_copy_bytes_per_launch, moe_peak_lds_read, moe_peak_lds_read_bytes_per_launch,
 )

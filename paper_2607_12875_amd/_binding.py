@@ -6,6 +6,7 @@ fallback of any kind: a missing library or a non-OK status raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -21,10 +22,15 @@ STATUS_NAMES = {0: "MOE_OK", 1: "MOE_ERR_NULL", 2: "MOE_ERR_SHAPE", 3: "MOE_ERR_
 SCORE = {"softmax": 0, "sigmoid": 1}
 WFMT = {"bf16": 0, "fp8": 1, "int4": 2, "fp8a16": 3, "mxfp4": 4, "mxfp4x8": 5}
 OFMT = {"f32": 0, "bf16": 1}
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+NORM = {"layer": 0, "rms": 1}
+ACT = {"silu": 0, "gelu": 1}
 
 EXPORTED = ("moe_status_str", "moe_permute_capacity", "moe_permute_workspace_bytes",
             "moe_gate_topk", "moe_router_gate_topk", "moe_router_workspace_bytes", "moe_permute", "moe_act_quant_fp8", "moe_workspace_bytes",
             "moe_workspace_layout", "moe_forward", "moe_forward_profiled", "moe_forward_static_ws",
+            "moe_norm_forward", "moe_norm_backward", "moe_norm_backward_workspace_bytes",
+            "moe_ffn_forward", "moe_ffn_backward", "moe_ffn_workspace_bytes", "moe_ffn_backward_workspace_bytes",
             # include/moe_peaks.h: achievable-peak probes
             "moe_peak_mfma_flops_per_launch", "moe_peak_sink_elems", "moe_peak_mfma", "moe_peak_read", "moe_peak_copy",
             "moe_peak_lds_copy_bytes_per_launch", "moe_peak_lds_copy", "moe_peak_lds_read_bytes_per_launch",
@@ -59,6 +65,11 @@ class MoeWsLayout(ctypes.Structure):
         "topk_ids", "topk_w", "expert_offsets", "sorted_ids", "inv_pos", "act_q", "act_s",
         "inter", "inter_s", "y", "permute_ws", "router_ws")] + [
         ("block_m", ctypes.c_int32), ("cap", ctypes.c_int32), ("total", ctypes.c_int64)]
+
+
+class MoeFfnArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "H", "I", "dtype", "act")] + [
+        (n, ctypes.c_void_p) for n in ("x", "w1", "w2", "add", "y", "pre", "dy", "dx", "dw1", "dw2")]
 
 
 _lib = None
@@ -118,6 +129,18 @@ def lib() -> ctypes.CDLL:
         L.moe_forward_profiled.restype = i32
         L.moe_forward_profiled.argtypes = [ctypes.POINTER(MoeArgs), vp, sz,
                                            ctypes.POINTER(ctypes.c_void_p), vp]
+        L.moe_norm_forward.restype = i32
+        L.moe_norm_forward.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp]
+        L.moe_norm_backward_workspace_bytes.restype = sz
+        L.moe_norm_backward_workspace_bytes.argtypes = [i32, i32]
+        L.moe_norm_backward.restype = i32
+        L.moe_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        for f in (L.moe_ffn_workspace_bytes, L.moe_ffn_backward_workspace_bytes):
+            f.restype = sz
+            f.argtypes = [ctypes.POINTER(MoeFfnArgs)]
+        for f in (L.moe_ffn_forward, L.moe_ffn_backward):
+            f.restype = i32
+            f.argtypes = [ctypes.POINTER(MoeFfnArgs), vp, sz, vp]
         _lib = L
     return _lib
 
@@ -289,6 +312,179 @@ def moe_forward(hidden, logits, w1, w2, top_k, *, mode="softmax", renormalize=Tr
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=hidden.device)
     moe_forward_args(args, workspace, stream)
     return out, workspace
+
+
+# ------------------------------------------------- norm, feed-forward block
+def _like(t, ref, name, shape=None, dtype=None):
+    """t is None, or a contiguous device tensor beside ref of that shape and type."""
+    if t is None:
+        return
+    if (not t.is_cuda or t.device != ref.device or not t.is_contiguous()
+            or t.shape != (ref.shape if shape is None else shape) or t.dtype != (ref.dtype if dtype is None else dtype)):
+        raise ValueError(f"{name}: expected a contiguous {dtype or ref.dtype} tensor of shape "
+                         f"{tuple(ref.shape if shape is None else shape)} on {ref.device}")
+
+
+def _rows(x, name):
+    if not x.is_cuda or not x.is_contiguous() or x.dim() != 2:
+        raise ValueError(f"{name}: expected a contiguous two-dimensional device tensor")
+    if x.dtype not in DTYPE:
+        raise ValueError(f"{name}: {x.dtype} is not supported")
+    return x.shape
+
+
+def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1e-5, y=None, sum_out=None,
+                     stats=True, stream=None):
+    """Layer or rms norm of the rows of x [T,H] (fp32, bf16, fp16), or of x +
+    residual: returns (y, s, mean, rstd).
+
+    s is what was normalised: x itself, or the sum rounded to the type (in
+    sum_out where given).  mean and rstd (fp32 [T], for moe_norm_backward) are
+    None without stats, mean also for "rms".  weight and bias [H] in x's type."""
+    T, H = _rows(x, "x")
+    _like(weight, x, "weight", (H,))
+    _like(bias, x, "bias", (H,))
+    _like(residual, x, "residual")
+    _like(y, x, "y")
+    _like(sum_out, x, "sum_out")
+    if y is None:
+        y = torch.empty_like(x)
+    if residual is None:
+        sum_out = None
+    elif sum_out is None:
+        sum_out = torch.empty_like(x)
+    mean = rstd = None
+    if stats:
+        rstd = torch.empty(T, dtype=torch.float32, device=x.device)
+        if kind != "rms":
+            mean = torch.empty_like(rstd)
+    with _on(x):
+        _check(lib().moe_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), T, H, NORM[kind],
+                                      DTYPE[x.dtype], float(eps), _ptr(y), _ptr(sum_out), _ptr(mean), _ptr(rstd),
+                                      _stream_of(x, stream)), "moe_norm_forward")
+    return y, x if residual is None else sum_out, mean, rstd
+
+
+def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=None, need_dweight=True,
+                      need_dbias=False, workspace=None, stream=None):
+    """Backward pass of moe_norm_forward: returns (dx, dweight, dbias), the last
+    two fp32 [H] or None.
+
+    x is the s that the forward pass returned, mean and rstd its statistics
+    (mean None for "rms"); dsum (or None) the gradient that reaches s on its
+    other way, added to dx.  workspace: a uint8 tensor of
+    moe_norm_backward_workspace_bytes, or None to allocate one."""
+    T, H = _rows(x, "x")
+    _like(dy, x, "dy")
+    _like(weight, x, "weight", (H,))
+    _like(mean, x, "mean", (T,), torch.float32)
+    _like(rstd, x, "rstd", (T,), torch.float32)
+    _like(dsum, x, "dsum")
+    _like(dx, x, "dx")
+    if dx is None:
+        dx = torch.empty_like(x)
+    dweight = torch.empty(H, dtype=torch.float32, device=x.device) if need_dweight else None
+    dbias = torch.empty(H, dtype=torch.float32, device=x.device) if need_dbias else None
+    nws = 0
+    if need_dweight or need_dbias:
+        nws = lib().moe_norm_backward_workspace_bytes(T, H)
+        workspace = _workspace(workspace, nws, x)
+    with _on(x):
+        _check(lib().moe_norm_backward(_ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dsum), T, H,
+                                       NORM[kind], DTYPE[x.dtype], _ptr(dx), _ptr(dweight), _ptr(dbias),
+                                       _ptr(workspace) if nws else None, nws, _stream_of(x, stream)),
+               "moe_norm_backward")
+    return dx, dweight, dbias
+
+
+def moe_norm_backward_workspace_bytes(T: int, H: int) -> int:
+    return lib().moe_norm_backward_workspace_bytes(T, H)
+
+
+def _workspace(ws, need, ref):
+    """ws if it holds need bytes on ref's device, else a new one."""
+    if ws is None or ws.numel() * ws.element_size() < need or ws.device != ref.device:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=ref.device)
+    if not ws.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return ws
+
+
+def _on(ref):
+    """The context of ref's device, where that is not the current one."""
+    return contextlib.nullcontext() if ref.device.index == torch.cuda.current_device() else torch.cuda.device(ref.device)
+
+
+def _stream_of(ref, stream):
+    s = torch.cuda.current_stream(ref.device) if stream is None else stream
+    return ctypes.c_void_p(s.cuda_stream)
+
+
+def make_ffn_args(T, H, I, *, dtype=torch.bfloat16, act="silu", x=None, w1=None, w2=None, add=None, y=None, pre=None,
+                  dy=None, dx=None, dw1=None, dw2=None) -> MoeFfnArgs:
+    return MoeFfnArgs(T, H, I, DTYPE[dtype], ACT[act], _ptr(x), _ptr(w1), _ptr(w2), _ptr(add), _ptr(y), _ptr(pre),
+                      _ptr(dy), _ptr(dx), _ptr(dw1), _ptr(dw2))
+
+
+def moe_ffn_workspace_bytes(args: MoeFfnArgs) -> int:
+    return lib().moe_ffn_workspace_bytes(ctypes.byref(args))
+
+
+def moe_ffn_backward_workspace_bytes(args: MoeFfnArgs) -> int:
+    return lib().moe_ffn_backward_workspace_bytes(ctypes.byref(args))
+
+
+def _ffn_shapes(x, w1, w2):
+    T, H = _rows(x, "x")
+    I = w2.shape[-1]
+    _like(w1, x, "w1", (2 * I, H))
+    _like(w2, x, "w2", (H, I))
+    return T, H, I
+
+
+def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=None, workspace=None, stream=None):
+    """Gated feed-forward block y = (act(x w1[:I]^T) * (x w1[I:]^T)) w2^T + add on
+    bf16 or fp16 x [T,H], w1 [2I,H], w2 [H,I] (H and I multiples of 8): returns
+    (y, pre, workspace).
+
+    With save, pre (fp32 [T,2I]) keeps both projections for moe_ffn_backward,
+    else it is None.  add [T,H] may be y itself."""
+    T, H, I = _ffn_shapes(x, w1, w2)
+    _like(add, x, "add")
+    _like(y, x, "y")
+    _like(pre, x, "pre", (T, 2 * I), torch.float32)
+    if y is None:
+        y = torch.empty_like(x)
+    if save and pre is None:
+        pre = torch.empty((T, 2 * I), dtype=torch.float32, device=x.device)
+    args = make_ffn_args(T, H, I, dtype=x.dtype, act=act, x=x, w1=w1, w2=w2, add=add, y=y, pre=pre)
+    workspace = _workspace(workspace, moe_ffn_workspace_bytes(args), x)
+    with _on(x):
+        _check(lib().moe_ffn_forward(ctypes.byref(args), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream_of(x, stream)), "moe_ffn_forward")
+    return y, pre, workspace
+
+
+def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=None, need=(True, True, True),
+                     workspace=None, stream=None):
+    """Backward pass of moe_ffn_forward from its pre: returns (dx, dw1, dw2,
+    workspace), the gradients in x's type.  need says which of them are
+    computed; the others are None."""
+    T, H, I = _ffn_shapes(x, w1, w2)
+    _like(dy, x, "dy")
+    _like(pre, x, "pre", (T, 2 * I), torch.float32)
+    _like(dx, x, "dx")
+    _like(dw1, x, "dw1", (2 * I, H))
+    _like(dw2, x, "dw2", (H, I))
+    dx = None if not need[0] else torch.empty_like(x) if dx is None else dx
+    dw1 = None if not need[1] else torch.empty_like(w1) if dw1 is None else dw1
+    dw2 = None if not need[2] else torch.empty_like(w2) if dw2 is None else dw2
+    args = make_ffn_args(T, H, I, dtype=x.dtype, act=act, x=x, w1=w1, w2=w2, pre=pre, dy=dy, dx=dx, dw1=dw1, dw2=dw2)
+    workspace = _workspace(workspace, moe_ffn_backward_workspace_bytes(args), x)
+    with _on(x):
+        _check(lib().moe_ffn_backward(ctypes.byref(args), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream_of(x, stream)), "moe_ffn_backward")
+    return dx, dw1, dw2, workspace
 
 
 # ------------------------------------------------------------ peak probes

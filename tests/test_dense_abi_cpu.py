@@ -1,0 +1,106 @@
+"""Refusals of the norm and the feed-forward block without a GPU: what the C ABI
+rejects on the host before any launch, workspace sizes, and the binding's checks."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2607_12875_amd as moe
+from paper_2607_12875_amd import _binding as B
+
+FAKE = 0x10000  # 16-byte aligned, never dereferenced on these paths
+
+
+def _norm(**kw):
+    a = dict(x=FAKE, residual=None, weight=FAKE, bias=None, T=4, H=64, kind=0, dtype=1, eps=1e-5, y=FAKE, sum=None,
+             mean=None, rstd=None)
+    a.update(kw)
+    return moe.lib().moe_norm_forward(*a.values(), None)
+
+
+def test_norm_forward_refusals():
+    assert _norm(T=0) == B.MOE_OK
+    assert _norm(T=-1) == _norm(T=(1 << 24) + 1) == _norm(H=0) == _norm(H=65537) == B.MOE_ERR_SHAPE
+    assert _norm(kind=2) == _norm(dtype=3) == _norm(eps=-1.0) == B.MOE_ERR_UNSUPPORTED
+    assert _norm(eps=float("nan")) == _norm(eps=float("inf")) == B.MOE_ERR_UNSUPPORTED
+    assert _norm(kind=1, bias=FAKE) == B.MOE_ERR_UNSUPPORTED
+    for k in ("x", "weight", "y"):
+        assert _norm(**{k: None}) == B.MOE_ERR_NULL
+    assert _norm(residual=FAKE) == B.MOE_ERR_NULL  # no place for the sum
+    for k in ("x", "residual", "weight", "bias", "y", "sum", "mean", "rstd"):
+        assert _norm(**{"sum": FAKE, k: FAKE + 4}) == B.MOE_ERR_ALIGN
+
+
+def _norm_back(**kw):
+    a = dict(dy=FAKE, x=FAKE, weight=FAKE, mean=FAKE, rstd=FAKE, dsum=None, T=4, H=64, kind=0, dtype=1, dx=FAKE,
+             dweight=FAKE, dbias=None, ws=FAKE, nbytes=1 << 30)
+    a.update(kw)
+    return moe.lib().moe_norm_backward(*a.values(), None)
+
+
+def test_norm_backward_refusals():
+    assert _norm_back(T=0, dweight=None) == B.MOE_OK
+    assert _norm_back(T=-1) == _norm_back(H=0) == B.MOE_ERR_SHAPE
+    assert _norm_back(kind=7) == _norm_back(dtype=-1) == _norm_back(kind=1, dbias=FAKE) == B.MOE_ERR_UNSUPPORTED
+    for k in ("dy", "x", "weight", "mean", "rstd", "dx"):
+        assert _norm_back(**{k: None}) == B.MOE_ERR_NULL
+    need = moe.moe_norm_backward_workspace_bytes(4, 64)
+    assert need >= 4 * 2 * 64 * 4
+    assert _norm_back(ws=None) == _norm_back(nbytes=need - 1) == B.MOE_ERR_WORKSPACE
+    for k in ("dy", "x", "weight", "mean", "rstd", "dsum", "dx", "dweight", "ws"):
+        assert _norm_back(**{k: FAKE + 8}) == B.MOE_ERR_ALIGN
+    assert moe.moe_norm_backward_workspace_bytes(-1, 64) == moe.moe_norm_backward_workspace_bytes(4, 1 << 17) == 0
+
+
+def _ffn(which="moe_ffn_forward", ws=FAKE, nbytes=1 << 40, null=False, **kw):
+    a = B.make_ffn_args(4, 64, 128)
+    for k in ("x", "w1", "w2", "y", "pre", "dy", "dx", "dw1", "dw2"):
+        setattr(a, k, FAKE)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return getattr(moe.lib(), which)(None if null else ctypes.byref(a), ws, nbytes, None)
+
+
+@pytest.mark.parametrize("which", ["moe_ffn_forward", "moe_ffn_backward"])
+def test_ffn_refusals(which):
+    assert _ffn(which, null=True) == B.MOE_ERR_NULL
+    for kw in (dict(T=-1), dict(T=(1 << 24) + 1), dict(H=0), dict(H=60), dict(I=4), dict(I=132), dict(H=65544), dict(I=1 << 17)):
+        assert _ffn(which, **kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(dtype=0), dict(dtype=3), dict(act=2), dict(act=-1)):
+        assert _ffn(which, **kw) == B.MOE_ERR_UNSUPPORTED, kw
+    reads = ("x", "w1", "w2", "y") if which == "moe_ffn_forward" else ("x", "w1", "w2", "dy", "pre")
+    for k in reads:
+        assert _ffn(which, **{k: None}) == B.MOE_ERR_NULL, k
+    for k in reads + (("add", "pre") if which == "moe_ffn_forward" else ("dx", "dw1", "dw2")):
+        assert _ffn(which, **{k: FAKE + 2}) == B.MOE_ERR_ALIGN, k
+    assert _ffn(which, ws=None) == _ffn(which, nbytes=16) == B.MOE_ERR_WORKSPACE
+    assert _ffn(which, ws=FAKE + 4) == B.MOE_ERR_ALIGN
+
+
+def test_ffn_nothing_to_do():
+    assert _ffn(T=0) == B.MOE_OK
+    assert _ffn("moe_ffn_backward", dx=None, dw1=None, dw2=None) == B.MOE_OK
+    # gradients that are not asked for need no inputs of their own
+    assert _ffn("moe_ffn_backward", dx=None, w1=None, ws=None) == B.MOE_ERR_WORKSPACE
+    assert _ffn("moe_ffn_backward", dw1=None, x=None, ws=None) == B.MOE_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("T", [0, 1, 7, 16, 33, 64, 100, 1000, 1025, 8192])
+@pytest.mark.parametrize("H,I", [(8, 8), (64, 4096), (4096, 1408), (7168, 2048)])
+def test_ffn_workspace_covers_the_intermediates(T, H, I):
+    a = B.make_ffn_args(T, H, I)
+    fwd, bwd = moe.moe_ffn_workspace_bytes(a), moe.moe_ffn_backward_workspace_bytes(a)
+    assert fwd >= T * I * 2 and bwd >= T * 3 * I * 2
+    assert fwd % 256 == bwd % 256 == 0
+    assert moe.moe_ffn_workspace_bytes(B.make_ffn_args(T, H + 4, I)) == 0
+    # partial products stay below what one pass over a few tiles of the chip gives
+    assert fwd <= T * I * 2 + (1 << 28) and bwd <= T * 3 * I * 2 + (1 << 28) + 512
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    w1, w2 = torch.zeros(256, 64, dtype=torch.bfloat16), torch.zeros(64, 128, dtype=torch.bfloat16)
+    for call in (lambda: moe.moe_norm_forward(x, x[0]), lambda: moe.moe_norm_backward(x, x, x[0], None, None),
+                 lambda: moe.moe_ffn_forward(x, w1, w2), lambda: moe.moe_ffn_backward(x, x, w1, w2, None)):
+        with pytest.raises(ValueError):  # host tensors
+            call()
