@@ -21,8 +21,10 @@ constexpr int kBK = 64;  // K elements per step: 128 bytes, one line of a row op
 
 // Sixteen bytes per lane from a bounds-checked buffer to LDS: lane l reads
 // offset voff and lands at `lds` + 16 l.  Lanes past the buffer's end write zeros.
+// The four wait states between the write of M0 and the copy (one is needed for M0)
+// also cover a descriptor word that the compiler took from a VGPR just before.
 __device__ __forceinline__ void bdma16(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
                : "memory", "m0");
 }
 __device__ __forceinline__ u32x4 buffer_of(uint64_t base, uint32_t bytes) {
@@ -49,56 +51,49 @@ struct Operand {
   static_assert(!COL || (R >= 64 && PARTS == 1), "column tiles");
   __device__ static int tswz(int k) { return R == 64 ? (k & 2) << 1 : (k & 3) << 2; }
 
-  uint64_t base[PARTS];
-  uint32_t left[PARTS];  // row: bytes from the base to the end of the tile's rows
+  uint64_t base[PARTS];  // where the next step starts
+  int left[PARTS];       // row: bytes from there to the end of the tile's rows; column: bytes before it in its row
   uint32_t voff[kCopies];
-  int ld;
+  u32x4 desc[PARTS];     // the step being copied
+  uint32_t past;         // row: all ones above the offsets where the lane's chunk lies past K
+  int ld, chunk;
 
   // row operand: `at` the first of `rows` rows that exist from the tile's start
   __device__ void rows(int part, const void* at, int rows, int ld_, int k0) {
     ld = ld_;
     base[part] = reinterpret_cast<uint64_t>(at) + static_cast<uint64_t>(k0) * 2;
-    left[part] = static_cast<uint32_t>(max(0, min(rows, R / PARTS))) * static_cast<uint32_t>(ld_) * 2u;
-    left[part] = left[part] ? left[part] - k0 * 2u : 0u;
+    left[part] = __builtin_amdgcn_readfirstlane(max(0, max(0, min(rows, R / PARTS)) * ld_ * 2 - k0 * 2));
   }
   // column operand: column m0 of the rows from k0 on
   __device__ void cols(const void* at, int m0, int ld_, int k0) {
     ld = ld_;
     base[0] = reinterpret_cast<uint64_t>(at) + (static_cast<uint64_t>(k0) * ld_ + m0) * 2;
-    left[0] = m0 * 2u;
+    left[0] = __builtin_amdgcn_readfirstlane(m0 * 2);
   }
   __device__ void offsets(int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int r = ((i % (kCopies / PARTS)) * NW + wave) * kRows + lane / kChunks;  // row within its part
       const int c = (lane % kChunks) ^ (COL ? tswz(r) : (r >> 1) & 7);
+      if (i == 0) chunk = c;
       voff[i] = static_cast<uint32_t>(r) * static_cast<uint32_t>(ld) * 2u + c * 16u;
     }
+    static_assert(COL || NW % 2 == 0, "a lane's chunk is the same in every copy");
   }
-  // The copies of the step that starts at k (of K), into LDS at `lds`; then
-  // the operand stands at the next step.
-  __device__ void issue(int k, int K, int wave, int lane, uint32_t lds) {
-    if constexpr (!COL) {
-      if (k + kBK > K) {  // uniform: the last step of a ragged K; chunks past K copy zeros
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int r = ((i % (kCopies / PARTS)) * NW + wave) * kRows + lane / kChunks;
-          const int c = (lane % kChunks) ^ ((r >> 1) & 7);
-          if (k + c * 8 >= K) voff[i] = 0x80000000u;
-        }
-      }
-    }
-    u32x4 d[PARTS];
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p)
-      d[p] = buffer_of(base[p], COL ? static_cast<uint32_t>(min(K - k, kBK)) * static_cast<uint32_t>(ld) * 2u - left[p] : left[p]);
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) bdma16(d[i / (kCopies / PARTS)], voff[i], lds + (i * NW + wave) * 1024);
+  // Make ready for the step that starts at k (of K; past its end the copies
+  // are zeros), and stand at the next one.
+  __device__ void step(int k, int K) {
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
+      desc[p] = buffer_of(base[p], COL ? max(0, max(0, min(K - k, kBK)) * ld * 2 - left[p]) : left[p]);
       base[p] += COL ? static_cast<uint64_t>(ld) * kBK * 2 : kBK * 2;
-      if (!COL) left[p] = left[p] > kBK * 2u ? left[p] - kBK * 2u : 0u;
+      if (!COL) left[p] = max(0, left[p] - kBK * 2);
     }
+    if (!COL) past = k + chunk * 8 >= K ? 0x80000000u : 0u;
+  }
+  // Copy i of that step into LDS at `lds`.
+  __device__ void copy(int i, int wave, uint32_t lds) const {
+    bdma16(desc[i / (kCopies / PARTS)], COL ? voff[i] : voff[i] | past, lds + (i * NW + wave) * 1024);
   }
   // Fragment of the 32 rows (columns) from r0 on at K substep kk: eight
   // consecutive k of group lane / 32 for row lane % 32.
@@ -121,39 +116,49 @@ struct Operand {
   }
 };
 
-// The epilogue on four columns of one row; SPLIT products come from the partial sums.
+// What an epilogue reads beside the products, for eight columns of one row.
+template <class E, int EPI> struct Beside {
+  f32x8 p, q;
+  __device__ void load(const DenseGemm& g, int m, int n) {
+    if constexpr (EPI == kStore) {
+      if (g.add) p = load8<E>(static_cast<const E*>(g.add) + static_cast<size_t>(m) * g.N + n);
+    } else if constexpr (EPI == kDglu) {
+      const float* at = g.pre_in + static_cast<size_t>(m) * 2 * g.N + n;
+      p = load8<float>(at);
+      q = load8<float>(at + g.N);
+    }
+  }
+};
+
+// The epilogue on eight columns of one row.
 template <class E, int EPI>
-__device__ __forceinline__ void finish4(const DenseGemm& g, int m, int n, const f32x4& c, const f32x4& up) {
+__device__ __forceinline__ void finish8(const DenseGemm& g, int m, int n, const f32x8& c, const f32x8& up, const Beside<E, EPI>& x) {
   const size_t at = static_cast<size_t>(m) * g.N + n;
   const size_t at2 = static_cast<size_t>(m) * 2 * g.N + n;
   if constexpr (EPI == kStore) {
-    f32x4 v = c;
-    if (g.add) v += load4<E>(static_cast<const E*>(g.add) + at);
-    store4<E>(static_cast<E*>(g.c) + at, v);
+    store8<E>(static_cast<E*>(g.c) + at, g.add ? c + x.p : c);
   } else if constexpr (EPI == kGlu) {
     if (g.pre) {
-      *reinterpret_cast<f32x4*>(g.pre + at2) = c;
-      *reinterpret_cast<f32x4*>(g.pre + at2 + g.N) = up;
+      store8<float>(g.pre + at2, c);
+      store8<float>(g.pre + at2 + g.N, up);
     }
-    f32x4 h;
+    f32x8 h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = act_of(g.act, c[i]) * up[i];
-    store4<E>(static_cast<E*>(g.c) + at, h);
+    for (int i = 0; i < 8; ++i) h[i] = act_of(g.act, c[i]) * up[i];
+    store8<E>(static_cast<E*>(g.c) + at, h);
   } else {
-    const f32x4 gt = *reinterpret_cast<const f32x4*>(g.pre_in + at2);
-    const f32x4 u = *reinterpret_cast<const f32x4*>(g.pre_in + at2 + g.N);
-    f32x4 dg, du, h;
+    f32x8 dg, du, h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
       float a, da;
-      act_and_slope(g.act, gt[i], a, da);
-      dg[i] = c[i] * u[i] * da;
+      act_and_slope(g.act, x.p[i], a, da);
+      dg[i] = c[i] * x.q[i] * da;
       du[i] = c[i] * a;
-      h[i] = a * u[i];
+      h[i] = a * x.q[i];
     }
-    store4<E>(static_cast<E*>(g.c) + at2, dg);
-    store4<E>(static_cast<E*>(g.c) + at2 + g.N, du);
-    if (g.h) store4<E>(static_cast<E*>(g.h) + at, h);
+    store8<E>(static_cast<E*>(g.c) + at2, dg);
+    store8<E>(static_cast<E*>(g.c) + at2 + g.N, du);
+    if (g.h) store8<E>(static_cast<E*>(g.h) + at, h);
   }
 }
 
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
   const int nk_all = (g.K + kBK - 1) / kBK;
   const int kt0 = static_cast<int>(static_cast<long>(nk_all) * split / splits);
   const int nk = static_cast<int>(static_cast<long>(nk_all) * (split + 1) / splits) - kt0;
-  const int k_first = kt0 * kBK;
+  const int k_first = kt0 * kBK, k_end = min(g.K, k_first + nk * kBK);
 
   A a;
   B b;
@@ -206,11 +211,14 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
     b.offsets(wave, lane);
   }
   const uint32_t smem0 = lds_addr(smem);
-  auto issue = [&](int kt) {
-    const uint32_t buf = smem0 + (kt % STAGES) * STAGE;
-    const int k = k_first + kt * kBK;
-    a.issue(k, g.K, wave, lane, buf);
-    b.issue(k, g.K, wave, lane, buf + A::kBytes);
+  // Copies [from, to) of stage kt: A's, then B's.
+  auto ready = [&](int kt) {
+    a.step(k_first + kt * kBK, k_end);
+    b.step(k_first + kt * kBK, k_end);
+  };
+  auto copy = [&](int i, uint32_t buf) {
+    if (i < A::kCopies) a.copy(i, wave, buf);
+    else b.copy(i - A::kCopies, wave, buf + A::kBytes);
   };
 
   f32x16 acc[TM][TN];
@@ -222,75 +230,117 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
   auto brow = [&](int j) { return DUAL ? (j < TN / 2 ? wn * (WTN / 2) + j * 32 : NC + wn * (WTN / 2) + (j - TN / 2) * 32) : wn * WTN + j * 32; };
 
   u32x4 fa[2][TM], fb[2][TN];
-  auto read = [&](int kt, int kk, int buf) {
-    const uint32_t at = smem0 + (kt % STAGES) * STAGE;
+  auto read = [&](uint32_t at, int kk, int buf) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) fa[buf][i] = A::frag(at, wm * WTM + i * 32, kk, lane);
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[buf][j] = B::frag(at + A::kBytes, brow(j), kk, lane);
   };
-  // at most `ahead` later steps' copies of this wave are still in flight
-  auto wait_ahead = [&](int ahead) {
-    if constexpr (STAGES >= 4) { if (ahead >= 3) { vm_wait<3 * N_DMA>(); return; } }
-    if constexpr (STAGES >= 3) { if (ahead == 2) { vm_wait<2 * N_DMA>(); return; } }
-    if (ahead == 1) { vm_wait<N_DMA>(); return; }
-    vm_wait<0>();
-  };
-
-  const int first = min(STAGES, nk);
-  for (int s = 0; s < first; ++s) issue(s);
-  wait_ahead(first - 1);
-  bar();
-  read(0, 0, 0);
-  constexpr int NKK = kBK / 16;
-  for (int kt = 0; kt < nk; ++kt) {
+  // The products of one substep, with copies [from, from + COUNT) spread between them.
+  auto multiply = [&](int buf, auto from, auto count, uint32_t dst) {
+    constexpr int FROM = decltype(from)::value, COUNT = decltype(count)::value, EVERY = COUNT ? (TM * TN + COUNT - 1) / COUNT : 1;
 #pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) {
-      if (kk + 1 < NKK) {
-        read(kt, kk + 1, (kk + 1) & 1);
-      } else if (kt + 1 < nk) {
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        lds_wait();  // this wave holds all of stage kt in registers
-        wait_ahead(min(STAGES - 2, nk - 2 - kt));
-        bar();  // stage kt + 1 has landed, stage kt's buffer is free
-        if (kt + STAGES < nk) issue(kt + STAGES);
-        read(kt + 1, 0, 0);
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int n = i * TN + j;
+        acc[i][j] = mfma32<E>(fb[buf][j], fa[buf][i], acc[i][j]);
+        if (n % EVERY == EVERY - 1 && n / EVERY < COUNT) {
+          __builtin_amdgcn_sched_barrier(0);
+          copy(FROM + n / EVERY, dst);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mfma32<E>(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
+    for (int c = TM * TN / EVERY; c < COUNT; ++c) copy(FROM + c, dst);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int NKK = kBK / 16, HALF = N_DMA / 2;
+  static_assert(NKK == 4 && N_DMA % 2 == 0, "substeps");
+  using std::integral_constant;
+  typedef integral_constant<int, 0> zero;
+  typedef integral_constant<int, HALF> half;
 
-  // Lane: row m0 + .. + lane % 32, four consecutive columns per quarter of the block.
+  // Stages 0 .. STAGES - 2 whole and half of the next; from then on each step
+  // copies the other half of its stage kt + STAGES - 1 and the first of the
+  // next.  Steps past the end copy zeros, so every wait counts the same.
+  uint32_t rd = smem0, wr = smem0;  // the buffers of stage kt and of the stage being copied
+  auto next = [&](uint32_t at) { return at + STAGE == smem0 + STAGES * STAGE ? smem0 : at + STAGE; };
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) {
+    ready(s);
+#pragma unroll
+    for (int i = 0; i < (s < STAGES - 1 ? N_DMA : HALF); ++i) copy(i, wr);
+    if (s < STAGES - 1) wr = next(wr);
+  }
+  vm_wait<(STAGES - 2) * N_DMA + HALF>();
+  bar();
+  read(rd, 0, 0);
+  for (int kt = 0; kt < nk; ++kt) {
+    read(rd, 1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(0, half{}, half{}, wr);
+    read(rd, 2, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1, zero{}, zero{}, wr);
+    read(rd, 3, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(0, zero{}, zero{}, wr);
+    ready(kt + STAGES);
+    wr = rd;
+    rd = next(rd);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    lds_wait();  // this wave holds all of stage kt in registers
+    vm_wait<(STAGES - 2) * N_DMA>();
+    bar();  // stage kt + 1 has landed, stage kt's buffer is free
+    read(rd, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(1, zero{}, half{}, wr);
+  }
+  vm_wait<0>();
+
+  // A wave turns its 32-row blocks over in LDS of its own, so that every load
+  // and store of the epilogue takes whole lines: eight columns per lane.
+  constexpr int PITCH = WTN + 4;  // floats per row: sixteen lanes' 16-byte writes lie in different banks
+  static_assert(NW * 32 * PITCH * 4 <= STAGES * STAGE, "the epilogue's rows fit the stages");
+  constexpr int LPR = WTN / (DUAL ? 16 : 8), RPI = 64 / LPR;  // lanes per row, rows per pass
+  bar();  // no wave reads the stages any more
+  float* const mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
+  const int er = lane / LPR, ec = lane % LPR * 8;
+  const int n = n0 + (DUAL ? wn * (WTN / 2) : wn * WTN) + ec;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + wm * WTM + i * 32 + (lane & 31);
-    if (m >= g.M) continue;
+    const int mb = m0 + wm * WTM + i * 32 + er;
+    Beside<E, EPI> x[32 / RPI];
+    if (!SPLIT && n < g.N) {
 #pragma unroll
-    for (int j = 0; j < (DUAL ? TN / 2 : TN); ++j) {
-      const int nb = n0 + brow(j) + 4 * (lane >> 5);
+      for (int r = 0; r < 32 / RPI; ++r)
+        if (mb + r * RPI < g.M) x[r].load(g, mb + r * RPI, n);
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int n = nb + 8 * q;
-        if (n >= g.N) continue;
-        f32x4 c, up{};
+        f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c[e] = acc[i][j][4 * q + e];
-          if (DUAL) up[e] = acc[i][j + (DUAL ? TN / 2 : 0)][4 * q + e];
-        }
-        if constexpr (SPLIT) {
-          const int w = DUAL ? 2 * g.N : g.N;
-          float* p = g.part + (static_cast<size_t>(split) * g.M + m) * w + n;
-          *reinterpret_cast<f32x4*>(p) = c;
-          if (DUAL) *reinterpret_cast<f32x4*>(p + g.N) = up;
-        } else {
-          finish4<E, EPI>(g, m, n, c, up);
-        }
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+        *reinterpret_cast<f32x4*>(mine + (lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
+      }
+#pragma unroll
+    for (int r = 0; r < 32 / RPI; ++r) {
+      const int m = mb + r * RPI;
+      if (m >= g.M || n >= g.N) continue;
+      const float* row = mine + (r * RPI + er) * PITCH + ec;
+      const f32x8 c = load8<float>(row);
+      f32x8 up{};
+      if constexpr (DUAL) up = load8<float>(row + WTN / 2);
+      if constexpr (SPLIT) {
+        const int w = DUAL ? 2 * g.N : g.N;
+        float* p = g.part + (static_cast<size_t>(split) * g.M + m) * w + n;
+        store8<float>(p, c);
+        if (DUAL) store8<float>(p + g.N, up);
+      } else {
+        finish8<E, EPI>(g, m, n, c, up, x[r]);
       }
     }
   }
@@ -300,17 +350,19 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
 template <class E, int EPI>
 __global__ __launch_bounds__(256) void dense_join_kernel(DenseGemm g, int splits) {
   constexpr bool DUAL = EPI == kGlu;
-  const size_t per_row = g.N / 4, n4 = static_cast<size_t>(g.M) * per_row;
+  const size_t per_row = g.N / 8, n8 = static_cast<size_t>(g.M) * per_row;
   const int w = DUAL ? 2 * g.N : g.N;
-  for (size_t i = blockIdx.x * 256ul + threadIdx.x; i < n4; i += gridDim.x * 256ul) {
-    const int m = static_cast<int>(i / per_row), n = static_cast<int>(i % per_row) * 4;
-    f32x4 c{}, up{};
+  for (size_t i = blockIdx.x * 256ul + threadIdx.x; i < n8; i += gridDim.x * 256ul) {
+    const int m = static_cast<int>(i / per_row), n = static_cast<int>(i % per_row) * 8;
+    Beside<E, EPI> x;
+    x.load(g, m, n);
+    f32x8 c{}, up{};
     for (int s = 0; s < splits; ++s) {
       const float* p = g.part + (static_cast<size_t>(s) * g.M + m) * w + n;
-      c += *reinterpret_cast<const f32x4*>(p);
-      if (DUAL) up += *reinterpret_cast<const f32x4*>(p + g.N);
+      c += load8<float>(p);
+      if (DUAL) up += load8<float>(p + g.N);
     }
-    finish4<E, EPI>(g, m, n, c, up);
+    finish8<E, EPI>(g, m, n, c, up, x);
   }
 }
 
@@ -350,8 +402,8 @@ hipError_t run_tile(const DenseGemm& g, int splits, hipStream_t s) {
   if (splits == 1) return go(dense_gemm_kernel<E, BM, BN, WM, WN, STAGES, ACOL, BCOL, EPI, false>);
   const hipError_t e = go(dense_gemm_kernel<E, BM, BN, WM, WN, STAGES, ACOL, BCOL, EPI, true>);
   if (e != hipSuccess) return e;
-  const size_t n4 = static_cast<size_t>(g.M) * (g.N / 4);
-  dense_join_kernel<E, EPI><<<static_cast<unsigned>(std::min<size_t>((n4 + 255) / 256, 2048)), 256, 0, s>>>(g, splits);
+  const size_t n8 = static_cast<size_t>(g.M) * (g.N / 8);
+  dense_join_kernel<E, EPI><<<static_cast<unsigned>(std::min<size_t>((n8 + 255) / 256, 2048)), 256, 0, s>>>(g, splits);
   return hipGetLastError();
 }
 

@@ -8,23 +8,31 @@ namespace moe {
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
-typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
-typedef f16_t f16x4 __attribute__((ext_vector_type(4)));
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
-template <class E> struct Vec4;
-template <> struct Vec4<bf16_t> { typedef bf16x4 type; };
-template <> struct Vec4<f16_t> { typedef f16x4 type; };
-template <> struct Vec4<float> { typedef f32x4 type; };
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <class E> struct Vec8;
+template <> struct Vec8<bf16_t> { typedef bf16x8 type; };
+template <> struct Vec8<f16_t> { typedef f16x8 type; };
 
-// Four consecutive elements (aligned to their size) to fp32 and back, rounded
-// to nearest even.
+// Eight consecutive elements (16-byte aligned) to fp32 and back, rounded to
+// nearest even.
 template <class E>
-__device__ __forceinline__ f32x4 load4(const E* p) {
-  return __builtin_convertvector(*reinterpret_cast<const typename Vec4<E>::type*>(p), f32x4);
+__device__ __forceinline__ f32x8 load8(const E* p) {
+  if constexpr (__is_same(E, float)) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else {
+    return __builtin_convertvector(*reinterpret_cast<const typename Vec8<E>::type*>(p), f32x8);
+  }
 }
 template <class E>
-__device__ __forceinline__ void store4(E* p, const f32x4& v) {
-  *reinterpret_cast<typename Vec4<E>::type*>(p) = __builtin_convertvector(v, typename Vec4<E>::type);
+__device__ __forceinline__ void store8(E* p, const f32x8& v) {
+  if constexpr (__is_same(E, float)) {
+    *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+    *reinterpret_cast<f32x4*>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+  } else {
+    *reinterpret_cast<typename Vec8<E>::type*>(p) = __builtin_convertvector(v, typename Vec8<E>::type);
+  }
 }
 
 // D(32x32, fp32) += A(32x16) * B(16x32); fragments and D as mfma32x32x16.
