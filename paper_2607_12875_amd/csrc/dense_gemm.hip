@@ -9,6 +9,7 @@
 // LDS as it lies.  A fragment of a row operand is one ds_read_b128; of a column
 // operand two ds_read_b64_tr_b16, which transpose 4 x 16 blocks on the way.
 #include <algorithm>
+#include <utility>
 
 #include "common.hpp"
 #include "dense.hpp"
@@ -20,12 +21,14 @@ namespace moe {
 constexpr int kBK = 64;  // K elements per step: 128 bytes, one line of a row operand
 
 // Sixteen bytes per lane from a bounds-checked buffer to LDS: lane l reads
-// offset voff and lands at `lds` + 16 l.  Lanes past the buffer's end write zeros.
-// The four wait states between the write of M0 and the copy (one is needed for M0)
-// also cover a descriptor word that the compiler took from a VGPR just before.
+// offset voff and lands at lds + AT + 16 l.  Lanes past the buffer's end write
+// zeros.  The four wait states between the write of M0 and the copy (one is
+// needed for M0) also cover a descriptor word that the compiler took from a VGPR
+// just before.
+template <int AT>
 __device__ __forceinline__ void bdma16(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
-               : "memory", "m0");
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc), "i"(AT)
+               : "memory", "m0", "scc");
 }
 __device__ __forceinline__ u32x4 buffer_of(uint64_t base, uint32_t bytes) {
   u32x4 r;
@@ -58,17 +61,21 @@ struct Operand {
   uint32_t past;         // row: all ones above the offsets where the lane's chunk lies past K
   int ld, chunk;
 
-  // row operand: `at` the first of `rows` rows that exist from the tile's start
-  __device__ void rows(int part, const void* at, int rows, int ld_, int k0) {
-    ld = ld_;
-    base[part] = reinterpret_cast<uint64_t>(at) + static_cast<uint64_t>(k0) * 2;
-    left[part] = __builtin_amdgcn_readfirstlane(max(0, max(0, min(rows, R / PARTS)) * ld_ * 2 - k0 * 2));
-  }
-  // column operand: column m0 of the rows from k0 on
-  __device__ void cols(const void* at, int m0, int ld_, int k0) {
-    ld = ld_;
-    base[0] = reinterpret_cast<uint64_t>(at) + (static_cast<uint64_t>(k0) * ld_ + m0) * 2;
-    left[0] = __builtin_amdgcn_readfirstlane(m0 * 2);
+  // The R rows (columns) from r0 on of an operand that has `count` of them, from
+  // k0 of K on.  Two parts: R / 2 from r0 and R / 2 from apart + r0 on.
+  __device__ void start(const void* at, int r0, int count, int K, int k0, int apart) {
+    const uint64_t first = reinterpret_cast<uint64_t>(at);
+    ld = COL ? count : K;
+    if constexpr (COL) {
+      base[0] = first + (static_cast<uint64_t>(k0) * ld + r0) * 2;
+      left[0] = __builtin_amdgcn_readfirstlane(r0 * 2);
+    } else {
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        base[p] = first + (static_cast<uint64_t>(r0 + p * apart) * ld + k0) * 2;
+        left[p] = __builtin_amdgcn_readfirstlane(max(0, max(0, min(count - r0, R / PARTS)) * ld * 2 - k0 * 2));
+      }
+    }
   }
   __device__ void offsets(int wave, int lane) {
 #pragma unroll
@@ -91,30 +98,51 @@ struct Operand {
     }
     if (!COL) past = k + chunk * 8 >= K ? 0x80000000u : 0u;
   }
-  // Copy i of that step into LDS at `lds`.
-  __device__ void copy(int i, int wave, uint32_t lds) const {
-    bdma16(desc[i / (kCopies / PARTS)], COL ? voff[i] : voff[i] | past, lds + (i * NW + wave) * 1024);
+  // Copy I of that step into LDS at `lds`, the buffer plus 1 KB per wave.
+  template <int I> __device__ void copy(uint32_t lds) const {
+    bdma16<I * NW * 1024>(desc[I / (kCopies / PARTS)], COL ? voff[I] : voff[I] | past, lds);
   }
-  // Fragment of the 32 rows (columns) from r0 on at K substep kk: eight
-  // consecutive k of group lane / 32 for row lane % 32.
-  __device__ static u32x4 frag(uint32_t lds, int r0, int kk, int lane) {
+
+  // Fragments, eight consecutive k of group lane / 32 of a K substep for row
+  // lane % 32 of a block of 32 rows: where this lane reads in a buffer, for the four
+  // substeps (row operand) or the four blocks from row r0 on (column operand; r0 a
+  // multiple of 128 where there are four), the rest is a constant.
+  __device__ static void lanes(uint32_t (&at)[4], int r0, int lane) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (!COL) {
+        const int r = r0 + (lane & 31);
+        at[q] = r * 128 + (((2 * q + (lane >> 5)) ^ ((r >> 1) & 7)) << 4);
+      } else {
+        // lane group of 16: columns 16 ((lane >> 4) & 1) .. of the block, rows 8 (lane >> 5) ..
+        const int k = (lane & 15) >> 2;  // and k + 4
+        const int c = r0 / 8 + 4 * q + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        at[q] = (8 * (lane >> 5) + k) * (R * 2) + ((c ^ tswz(k)) << 4) + ((lane & 1) << 3);
+      }
+    }
+  }
+  // Block `i` (rows apart: `rows`) at substep kk; at[] with the buffer's address added.
+  __device__ static u32x4 frag(const uint32_t (&at)[4], int i, int rows, int kk) {
     if constexpr (!COL) {
-      const int r = r0 + (lane & 31);
-      return lds16(lds + r * 128 + (((2 * kk + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
+      return lds16(at[kk] + rows * 128);
     } else {
-      // lane group of 16: columns 16 ((lane >> 4) & 1) .. of the block, rows 8 (lane >> 5) ..
-      const int k = (lane & 15) >> 2;  // and k + 4
-      const int c = r0 / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      const uint32_t at = lds + (16 * kk + 8 * (lane >> 5) + k) * (R * 2) + ((c ^ tswz(k)) << 4) + ((lane & 1) << 3);
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s16x4* lp;
-      const i32x2 lo = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)at));
-      const i32x2 hi = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(at + 4 * R * 2)));
+      const uint32_t p = at[i] + 16 * kk * (R * 2);
+      const i32x2 lo = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p));
+      const i32x2 hi = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * R * 2)));
       return u32x4{static_cast<uint32_t>(lo.x), static_cast<uint32_t>(lo.y), static_cast<uint32_t>(hi.x),
                    static_cast<uint32_t>(hi.y)};
     }
   }
 };
+
+// f(integral_constant<int, 0>) .. f(integral_constant<int, N - 1>)
+template <class F, int... I>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F f) { each(std::make_integer_sequence<int, N>{}, f); }
 
 // What an epilogue reads beside the products, for eight columns of one row.
 template <class E, int EPI> struct Beside {
@@ -162,155 +190,58 @@ __device__ __forceinline__ void finish8(const DenseGemm& g, int m, int n, const 
   }
 }
 
-// Workgroup tile BM x BN (kGlu: BN / 2 gate and BN / 2 up rows of B) in WM x WN
-// waves; STAGES buffers of kBK.  Stage kt + STAGES goes into the buffer of stage
-// kt once every wave has read it (the barrier in the last substep of step kt).
-template <class E, int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, int EPI, bool SPLIT>
-__global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
-  constexpr int NW = WM * WN;
-  constexpr bool DUAL = EPI == kGlu;
-  constexpr int NC = DUAL ? BN / 2 : BN;  // columns of C per tile
-  using A = Operand<BM, ACOL, NW, 1>;
-  using B = Operand<BN, BCOL, NW, DUAL ? 2 : 1>;
-  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
-  static_assert(!DUAL || TN % 2 == 0, "gate and up pairs");
-  constexpr int STAGE = A::kBytes + B::kBytes, N_DMA = A::kCopies + B::kCopies;
-  static_assert((STAGES - 1) * N_DMA < 64, "vmcnt range");
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / WN, wn = wave % WN;
-  // Workgroups land on the XCDs in turn: each XCD takes one contiguous range of
-  // tiles, column by column over groups of eight row tiles.
+// The part of the product that a workgroup computes.
+struct Place {
+  int m0, n0, split, k_first, k_end, nk;
+};
+// Workgroups land on the XCDs in turn: each XCD takes one contiguous range of
+// tiles, column by column over groups of eight row tiles.  False: nothing left.
+template <int BM, int NC>
+__device__ __forceinline__ bool place_of(const DenseGemm& g, int tiles_m, int tiles_n, int splits, Place& p) {
   const int total = tiles_m * tiles_n * splits;
   const int per = (total + 7) / 8;
   int t = (blockIdx.x % 8) * per + blockIdx.x / 8;
-  if (t >= total || static_cast<int>(blockIdx.x / 8) >= per) return;
-  const int split = t / (tiles_m * tiles_n);
+  if (t >= total || static_cast<int>(blockIdx.x / 8) >= per) return false;
+  p.split = t / (tiles_m * tiles_n);
   t %= tiles_m * tiles_n;
   constexpr int GM = 8;
   const int grp = t / (GM * tiles_n), in = t % (GM * tiles_n), gsz = min(GM, tiles_m - grp * GM);
-  const int m0 = (grp * GM + in % gsz) * BM, n0 = (in / gsz) * NC;
-
+  p.m0 = (grp * GM + in % gsz) * BM;
+  p.n0 = (in / gsz) * NC;
   const int nk_all = (g.K + kBK - 1) / kBK;
-  const int kt0 = static_cast<int>(static_cast<long>(nk_all) * split / splits);
-  const int nk = static_cast<int>(static_cast<long>(nk_all) * (split + 1) / splits) - kt0;
-  const int k_first = kt0 * kBK, k_end = min(g.K, k_first + nk * kBK);
+  const int kt0 = static_cast<int>(static_cast<long>(nk_all) * p.split / splits);
+  p.nk = static_cast<int>(static_cast<long>(nk_all) * (p.split + 1) / splits) - kt0;
+  p.k_first = kt0 * kBK;
+  p.k_end = min(g.K, p.k_first + p.nk * kBK);
+  return true;
+}
 
-  A a;
-  B b;
-  {
-    const uint16_t* pa = static_cast<const uint16_t*>(g.a);
-    const uint16_t* pb = static_cast<const uint16_t*>(g.b);
-    if constexpr (ACOL) a.cols(pa, m0, g.M, k_first);
-    else a.rows(0, pa + static_cast<size_t>(m0) * g.K, g.M - m0, g.K, k_first);
-    if constexpr (BCOL) b.cols(pb, n0, g.N, k_first);
-    else b.rows(0, pb + static_cast<size_t>(n0) * g.K, g.N - n0, g.K, k_first);
-    if constexpr (DUAL) b.rows(1, pb + (static_cast<size_t>(g.N) + n0) * g.K, g.N - n0, g.K, k_first);
-    a.offsets(wave, lane);
-    b.offsets(wave, lane);
-  }
-  const uint32_t smem0 = lds_addr(smem);
-  // Copies [from, to) of stage kt: A's, then B's.
-  auto ready = [&](int kt) {
-    a.step(k_first + kt * kBK, k_end);
-    b.step(k_first + kt * kBK, k_end);
-  };
-  auto copy = [&](int i, uint32_t buf) {
-    if (i < A::kCopies) a.copy(i, wave, buf);
-    else b.copy(i - A::kCopies, wave, buf + A::kBytes);
-  };
+// The waves of a tile: WM x WN of them, TM x TN blocks of 32 x 32 each.
+template <int BM, int BN, int WM, int WN, int EPI> struct Waves {
+  static constexpr bool DUAL = EPI == kGlu;
+  static constexpr int NW = WM * WN, NC = DUAL ? BN / 2 : BN;  // NC: columns of C per tile
+  static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
+  static_assert(!DUAL || TN % 2 == 0, "gate and up pairs");
+  static constexpr int PITCH = WTN + 4;  // floats per row of the epilogue: sixteen lanes' 16-byte writes lie in different banks
+  static constexpr int kEpilogueBytes = NW * 32 * PITCH * 4;
+  // first B row of wave column wn, and the rows from there to its block j
+  __device__ static int bfirst(int wn) { return wn * (DUAL ? WTN / 2 : WTN); }
+  __device__ static constexpr int brows(int j) { return DUAL && j >= TN / 2 ? NC + (j - TN / 2) * 32 : j * 32; }
+};
 
-  f32x16 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
-  // B row (within the tile) of wave tile j
-  auto brow = [&](int j) { return DUAL ? (j < TN / 2 ? wn * (WTN / 2) + j * 32 : NC + wn * (WTN / 2) + (j - TN / 2) * 32) : wn * WTN + j * 32; };
-
-  u32x4 fa[2][TM], fb[2][TN];
-  auto read = [&](uint32_t at, int kk, int buf) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) fa[buf][i] = A::frag(at, wm * WTM + i * 32, kk, lane);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) fb[buf][j] = B::frag(at + A::kBytes, brow(j), kk, lane);
-  };
-  // The products of one substep, with copies [from, from + COUNT) spread between them.
-  auto multiply = [&](int buf, auto from, auto count, uint32_t dst) {
-    constexpr int FROM = decltype(from)::value, COUNT = decltype(count)::value, EVERY = COUNT ? (TM * TN + COUNT - 1) / COUNT : 1;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = i * TN + j;
-        acc[i][j] = mfma32<E>(fb[buf][j], fa[buf][i], acc[i][j]);
-        if (n % EVERY == EVERY - 1 && n / EVERY < COUNT) {
-          __builtin_amdgcn_sched_barrier(0);
-          copy(FROM + n / EVERY, dst);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-#pragma unroll
-    for (int c = TM * TN / EVERY; c < COUNT; ++c) copy(FROM + c, dst);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  constexpr int NKK = kBK / 16, HALF = N_DMA / 2;
-  static_assert(NKK == 4 && N_DMA % 2 == 0, "substeps");
-  using std::integral_constant;
-  typedef integral_constant<int, 0> zero;
-  typedef integral_constant<int, HALF> half;
-
-  // Stages 0 .. STAGES - 2 whole and half of the next; from then on each step
-  // copies the other half of its stage kt + STAGES - 1 and the first of the
-  // next.  Steps past the end copy zeros, so every wait counts the same.
-  uint32_t rd = smem0, wr = smem0;  // the buffers of stage kt and of the stage being copied
-  auto next = [&](uint32_t at) { return at + STAGE == smem0 + STAGES * STAGE ? smem0 : at + STAGE; };
-#pragma unroll
-  for (int s = 0; s < STAGES; ++s) {
-    ready(s);
-#pragma unroll
-    for (int i = 0; i < (s < STAGES - 1 ? N_DMA : HALF); ++i) copy(i, wr);
-    if (s < STAGES - 1) wr = next(wr);
-  }
-  vm_wait<(STAGES - 2) * N_DMA + HALF>();
-  bar();
-  read(rd, 0, 0);
-  for (int kt = 0; kt < nk; ++kt) {
-    read(rd, 1, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(0, half{}, half{}, wr);
-    read(rd, 2, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(1, zero{}, zero{}, wr);
-    read(rd, 3, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(0, zero{}, zero{}, wr);
-    ready(kt + STAGES);
-    wr = rd;
-    rd = next(rd);
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    lds_wait();  // this wave holds all of stage kt in registers
-    vm_wait<(STAGES - 2) * N_DMA>();
-    bar();  // stage kt + 1 has landed, stage kt's buffer is free
-    read(rd, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(1, zero{}, half{}, wr);
-  }
-  vm_wait<0>();
-
-  // A wave turns its 32-row blocks over in LDS of its own, so that every load
-  // and store of the epilogue takes whole lines: eight columns per lane.
-  constexpr int PITCH = WTN + 4;  // floats per row: sixteen lanes' 16-byte writes lie in different banks
-  static_assert(NW * 32 * PITCH * 4 <= STAGES * STAGE, "the epilogue's rows fit the stages");
+// A wave turns its 32-row blocks over in LDS of its own, so that every load and
+// store of the epilogue takes whole lines: eight columns per lane.
+template <class E, class W, int EPI, bool SPLIT>
+__device__ __forceinline__ void epilogue(const DenseGemm& g, const Place& p, int wm, int wn, int lane, float* mine,
+                                         const f32x16 (&acc)[W::TM][W::TN]) {
+  constexpr bool DUAL = W::DUAL;
+  constexpr int PITCH = W::PITCH, WTN = W::WTN;
   constexpr int LPR = WTN / (DUAL ? 16 : 8), RPI = 64 / LPR;  // lanes per row, rows per pass
-  bar();  // no wave reads the stages any more
-  float* const mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
   const int er = lane / LPR, ec = lane % LPR * 8;
-  const int n = n0 + (DUAL ? wn * (WTN / 2) : wn * WTN) + ec;
+  const int n = p.n0 + (DUAL ? wn * (WTN / 2) : wn * WTN) + ec;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int mb = m0 + wm * WTM + i * 32 + er;
+  for (int i = 0; i < W::TM; ++i) {
+    const int mb = p.m0 + wm * W::WTM + i * 32 + er;
     Beside<E, EPI> x[32 / RPI];
     if (!SPLIT && n < g.N) {
 #pragma unroll
@@ -318,7 +249,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
         if (mb + r * RPI < g.M) x[r].load(g, mb + r * RPI, n);
     }
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < W::TN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         f32x4 v;
@@ -336,14 +267,242 @@ __global__ __launch_bounds__(WM * WN * 64, BM == 256 ? 2 : 2) void dense_gemm_ke
       if constexpr (DUAL) up = load8<float>(row + WTN / 2);
       if constexpr (SPLIT) {
         const int w = DUAL ? 2 * g.N : g.N;
-        float* p = g.part + (static_cast<size_t>(split) * g.M + m) * w + n;
-        store8<float>(p, c);
-        if (DUAL) store8<float>(p + g.N, up);
+        float* at = g.part + (static_cast<size_t>(p.split) * g.M + m) * w + n;
+        store8<float>(at, c);
+        if (DUAL) store8<float>(at + g.N, up);
       } else {
         finish8<E, EPI>(g, m, n, c, up, x[r]);
       }
     }
   }
+}
+
+// A wave's fragments, for this K substep and the next, and its products.
+template <class E, class W, class A, class B> struct Math {
+  static constexpr int TM = W::TM, TN = W::TN, N = TM * TN, R = TM + TN;
+  u32x4 fa[2][TM], fb[2][TN];
+  f32x16 acc[TM][TN];
+  uint32_t la[4], lb[4], pa[4], pb[4];  // where the lane reads in a buffer, and in the buffers being read
+  __device__ void start(int a0, int b0, int lane) {
+    A::lanes(la, a0, lane);
+    B::lanes(lb, b0, lane);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
+  }
+  __device__ void from(uint32_t at_a, uint32_t at_b) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      pa[q] = la[q] + at_a;
+      pb[q] = lb[q] + at_b;
+    }
+  }
+  // fragment r of substep kk, in the order that the products want them
+  __device__ void read(int kk, int r) {
+    if (r < TN) fb[kk & 1][r] = B::frag(pb, r, W::brows(r), kk);
+    else fa[kk & 1][r - TN] = A::frag(pa, r - TN, (r - TN) * 32, kk);
+  }
+  __device__ void read(int kk) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) read(kk, r);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // substep kk's products; work(n) after the nth
+  template <class F> __device__ void multiply(int kk, F work) {
+    each<N>([&](auto n) {
+      constexpr int i = n / TN, j = n % TN;
+      acc[i][j] = mfma32<E>(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      work(n);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  }
+  __device__ void multiply(int kk) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) acc[n / TN][n % TN] = mfma32<E>(fb[kk & 1][n % TN], fa[kk & 1][n / TN], acc[n / TN][n % TN]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// Before a barrier that frees a buffer: this wave's fragments of it have arrived,
+// and at most N of its copies are still in flight.
+template <int N>
+__device__ __forceinline__ void settle() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  lds_wait();
+  vm_wait<N>();
+}
+
+// Workgroup tile BM x BN (kGlu: BN / 2 gate and BN / 2 up rows of B) in WM x WN
+// waves; STAGES buffers of kBK.  Stage kt + STAGES goes into the buffer of stage
+// kt once every wave has read it (the barrier before the last substep of step
+// kt): half of its copies in that substep, half in the next.  Steps past the end
+// copy zeros, so there is no branch in the loop and every wait counts the same.
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void dense_gemm_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+  using W = Waves<BM, BN, WM, WN, EPI>;
+  using A = Operand<BM, ACOL, W::NW, 1>;
+  using B = Operand<BN, BCOL, W::NW, W::DUAL ? 2 : 1>;
+  constexpr int STAGE = A::kBytes + B::kBytes, N_DMA = A::kCopies + B::kCopies, HALF = N_DMA / 2;
+  static_assert(N_DMA % 2 == 0 && (STAGES - 1) * N_DMA < 64 && W::kEpilogueBytes <= STAGES * STAGE, "stages");
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+
+  Place p;
+  if (!place_of<BM, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  A a;
+  B b;
+  a.start(g.a, p.m0, g.M, g.K, p.k_first, 0);
+  b.start(g.b, p.n0, g.N, g.K, p.k_first, g.N);
+  a.offsets(wave, lane);
+  b.offsets(wave, lane);
+  auto ready = [&](int kt) {
+    a.step(p.k_first + kt * kBK, p.k_end);
+    b.step(p.k_first + kt * kBK, p.k_end);
+  };
+  const uint32_t smem0 = lds_addr(smem), mine = wave * 1024;
+  auto copy = [&](auto i, uint32_t buf) {
+    if constexpr (i < A::kCopies) a.template copy<i>(buf + mine);
+    else b.template copy<i - A::kCopies>(buf + A::kBytes + mine);
+  };
+  uint32_t rd = smem0, wr = smem0;  // the buffers of stage kt and of the stage being copied
+  auto next = [&](uint32_t at) { return at + STAGE == smem0 + STAGES * STAGE ? smem0 : at + STAGE; };
+  Math<E, W, A, B> x;
+  x.start(wm * W::WTM, W::bfirst(wn), lane);
+  // copies FROM .. FROM + HALF - 1 spread over a substep's products
+  auto spread = [&](int kk, auto from) {
+    constexpr int EVERY = (x.N + HALF - 1) / HALF;
+    x.multiply(kk, [&](auto n) {
+      if constexpr (n % EVERY == EVERY - 1 && n / EVERY < HALF) copy(std::integral_constant<int, from + n / EVERY>{}, wr);
+      if constexpr (n == x.N - 1)
+        each<HALF>([&](auto c) {
+          if constexpr (c >= x.N / EVERY) copy(std::integral_constant<int, from + c>{}, wr);
+        });
+    });
+  };
+  typedef std::integral_constant<int, 0> first_half;
+  typedef std::integral_constant<int, HALF> second_half;
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    ready(s);
+    each<N_DMA>([&](auto i) { copy(i, wr); });
+    wr = next(wr);
+  }
+  ready(STAGES - 1);
+  each<HALF>([&](auto i) { copy(i, wr); });
+  vm_wait<(STAGES - 2) * N_DMA + HALF>();
+  bar();
+  x.from(rd, rd + A::kBytes);
+  x.read(0);
+  for (int kt = 0; kt < p.nk; ++kt) {
+    x.read(1);
+    spread(0, second_half{});
+    x.read(2);
+    x.multiply(1);
+    x.read(3);
+    x.multiply(2);
+    ready(kt + STAGES);
+    wr = rd;
+    rd = next(rd);
+    x.from(rd, rd + A::kBytes);
+    settle<(STAGES - 2) * N_DMA>();
+    bar();  // stage kt + 1 has landed, stage kt's buffer is free
+    x.read(0);
+    spread(3, first_half{});
+  }
+  vm_wait<0>();
+  bar();  // no wave reads the stages any more, no copy is under way
+  epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
+}
+
+// 256 x 256 tile, four waves of 128 x 128, each with a SIMD to itself (the sums
+// take half of its 512 registers).  The LDS reads of the products are the fewest
+// that way, 128 KB per step; with the 64 KB that land they take most of the LDS's
+// time, so they are spread evenly: after a substep's sixteen products come, in
+// turn, a fragment of the next substep and, every fourth time, a copy.  A has two
+// buffers, B three, all of the 160 KB: A's copies follow the barrier that frees
+// their buffer, B's, for a stage further on, come in the half step after, so that
+// no copy has less than three quarters of a step to land.  8192 tokens, 4096 x
+// 11264: y = h W2^T runs the matrix pipe 75 % of the cycles (67 with eight waves of
+// 128 x 64 in two groups half a step apart, 61 with eight in step), dx 79 %.
+template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+__global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+  using W = Waves<256, 256, 2, 2, EPI>;
+  using A = Operand<256, ACOL, 4, 1>;
+  using B = Operand<256, BCOL, 4, W::DUAL ? 2 : 1>;
+  constexpr int NA = A::kCopies, NB = B::kCopies;
+  static_assert(NA == 8 && NB == 8 && W::kEpilogueBytes <= 2 * A::kBytes + 3 * B::kBytes, "four copies per substep");
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+
+  Place p;
+  if (!place_of<256, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / 2, wn = wave % 2;
+  A a;
+  B b;
+  a.start(g.a, p.m0, g.M, g.K, p.k_first, 0);
+  b.start(g.b, p.n0, g.N, g.K, p.k_first, g.N);
+  a.offsets(wave, lane);
+  b.offsets(wave, lane);
+  const uint32_t a0 = lds_addr(smem), b0 = a0 + 2 * A::kBytes, mine = wave * 1024;
+  uint32_t ra = a0, rb = b0, wa = a0, wb = b0;  // buffers being read and written
+  auto next_a = [&](uint32_t at) { return at == a0 ? a0 + A::kBytes : a0; };
+  auto next_b = [&](uint32_t at) { return at == b0 + 2 * B::kBytes ? b0 : at + B::kBytes; };
+  auto ready_a = [&](int kt) { a.step(p.k_first + kt * kBK, p.k_end); };
+  auto ready_b = [&](int kt) { b.step(p.k_first + kt * kBK, p.k_end); };
+  Math<E, W, A, B> x;
+  x.start(wm * W::WTM, W::bfirst(wn), lane);
+  // substep kk, the next one's fragments, and four copies
+  auto substep = [&](int kk, auto copy) {
+    x.multiply(kk, [&](auto n) {
+      if constexpr (n % 2 == 0) x.read((kk + 1) % 4, n / 2);
+      else if constexpr (n % 4 == 1) copy(std::integral_constant<int, n / 4>{});
+    });
+  };
+  auto a_low = [&](auto c) { a.template copy<c>(wa + mine); };
+  auto a_high = [&](auto c) { a.template copy<c + 4>(wa + mine); };
+  auto b_low = [&](auto c) { b.template copy<c>(wb + mine); };
+  auto b_high = [&](auto c) { b.template copy<c + 4>(wb + mine); };
+
+  // stages 0 and 1, B first; then B's stage 2 before A's, as in the loop
+  ready_b(0);
+  each<NB>([&](auto i) { b.template copy<i>(wb + mine); });
+  wb = next_b(wb);
+  ready_a(0);
+  each<NA>([&](auto i) { a.template copy<i>(wa + mine); });
+  wa = next_a(wa);
+  ready_b(1);
+  each<NB>([&](auto i) { b.template copy<i>(wb + mine); });
+  wb = next_b(wb);
+  ready_a(1);
+  each<NA>([&](auto i) { a.template copy<i>(wa + mine); });
+  vm_wait<NA + NB>();
+  bar();
+  x.from(ra, rb);
+  x.read(0);
+  ready_b(2);
+  for (int kt = 0; kt < p.nk; ++kt) {
+    // here: A's stage kt + 1 has gone out, of B's stage kt + 2 nothing yet
+    substep(0, b_low);
+    substep(1, b_high);
+    wb = next_b(wb);
+    wa = ra;
+    ra = next_a(ra);
+    rb = next_b(rb);
+    ready_a(kt + 2);
+    substep(2, [](auto) {});
+    x.from(ra, rb);
+    settle<NB>();
+    bar();  // stage kt + 1 has landed, stage kt's buffers are free
+    substep(3, [&](auto c) { a.template copy<c>(wa + mine); a.template copy<c + 4>(wa + mine); });
+    ready_b(kt + 3);
+  }
+  vm_wait<0>();
+  bar();  // no wave reads the stages any more, no copy is under way
+  epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
 }
 
 // The partial products of a split K, added in the order of the splits, and the epilogue.
@@ -386,22 +545,20 @@ Plan plan_for(int epi, int M, int N, int K) {
   return p;
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, int EPI>
-hipError_t run_tile(const DenseGemm& g, int splits, hipStream_t s) {
+// Launches a tile kernel, the whole of K or one of its splits per workgroup, and
+// what joins the splits.
+template <class E, int BM, int BN, int NW, int LDS, int EPI, class K>
+hipError_t run_tile(const DenseGemm& g, int splits, K whole, K part, hipStream_t s) {
   constexpr int NC = EPI == kGlu ? BN / 2 : BN;
-  constexpr int lds = STAGES * (BM + BN) * kBK * 2;
   const int tm = (g.M + BM - 1) / BM, tn = (g.N + NC - 1) / NC;
   const long total = static_cast<long>(tm) * tn * splits;
-  const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8)), block(WM * WN * 64);
-  auto go = [&](auto kernel) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    kernel<<<grid, block, lds, s>>>(g, tm, tn, splits);
-    return hipGetLastError();
-  };
-  if (splits == 1) return go(dense_gemm_kernel<E, BM, BN, WM, WN, STAGES, ACOL, BCOL, EPI, false>);
-  const hipError_t e = go(dense_gemm_kernel<E, BM, BN, WM, WN, STAGES, ACOL, BCOL, EPI, true>);
+  const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8)), block(NW * 64);
+  const K kernel = splits == 1 ? whole : part;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (e != hipSuccess) return e;
+  kernel<<<grid, block, LDS, s>>>(g, tm, tn, splits);
+  e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
   const size_t n8 = static_cast<size_t>(g.M) * (g.N / 8);
   dense_join_kernel<E, EPI><<<static_cast<unsigned>(std::min<size_t>((n8 + 255) / 256, 2048)), 256, 0, s>>>(g, splits);
   return hipGetLastError();
@@ -410,9 +567,14 @@ hipError_t run_tile(const DenseGemm& g, int splits, hipStream_t s) {
 template <class E, bool ACOL, bool BCOL, int EPI>
 hipError_t run(const DenseGemm& g, hipStream_t s) {
   const Plan p = plan_for(EPI, g.M, g.N, g.K);
-  if (p.tile == 256) return run_tile<E, 256, 256, 2, 4, 2, ACOL, BCOL, EPI>(g, p.splits, s);
-  if (p.tile == 128) return run_tile<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI>(g, p.splits, s);
-  return run_tile<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI>(g, p.splits, s);
+  if (p.tile == 256)
+    return run_tile<E, 256, 256, 4, 160 * 1024, EPI>(g, p.splits, dense_gemm_256_kernel<E, ACOL, BCOL, EPI, false>,
+                                                     dense_gemm_256_kernel<E, ACOL, BCOL, EPI, true>, s);
+  if (p.tile == 128)
+    return run_tile<E, 128, 128, 4, 64 * 1024, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, false>,
+                                                    dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, true>, s);
+  return run_tile<E, 64, 128, 4, 72 * 1024, EPI>(g, p.splits, dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
+                                                 dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
 }
 
 template <class E>
