@@ -55,4 +55,8 @@ enum DenseLayout { kRowRow, kRowCol, kColCol };
 size_t dense_gemm_workspace_bytes(int layout, int epi, int M, int N, int K);
 hipError_t launch_dense_gemm(int dtype, int layout, int epi, const DenseGemm& g, hipStream_t s);
 
+// The forward products for few rows of A, where that is the faster form.
+bool dense_rows_fits(int layout, int epi, int M, int N, int K);
+hipError_t launch_dense_rows(int dtype, int epi, const DenseGemm& g, hipStream_t s);
+
 }  // namespace moe

@@ -13,6 +13,7 @@
 
 #include "common.hpp"
 #include "dense.hpp"
+#include "dense_finish.hpp"
 #include "dense_math.hpp"
 #include "lds_dma.hpp"
 
@@ -143,52 +144,6 @@ __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f) {
   (f(std::integral_constant<int, I>{}), ...);
 }
 template <int N, class F> __device__ __forceinline__ void each(F f) { each(std::make_integer_sequence<int, N>{}, f); }
-
-// What an epilogue reads beside the products, for eight columns of one row.
-template <class E, int EPI> struct Beside {
-  f32x8 p, q;
-  __device__ void load(const DenseGemm& g, int m, int n) {
-    if constexpr (EPI == kStore) {
-      if (g.add) p = load8<E>(static_cast<const E*>(g.add) + static_cast<size_t>(m) * g.N + n);
-    } else if constexpr (EPI == kDglu) {
-      const float* at = g.pre_in + static_cast<size_t>(m) * 2 * g.N + n;
-      p = load8<float>(at);
-      q = load8<float>(at + g.N);
-    }
-  }
-};
-
-// The epilogue on eight columns of one row.
-template <class E, int EPI>
-__device__ __forceinline__ void finish8(const DenseGemm& g, int m, int n, const f32x8& c, const f32x8& up, const Beside<E, EPI>& x) {
-  const size_t at = static_cast<size_t>(m) * g.N + n;
-  const size_t at2 = static_cast<size_t>(m) * 2 * g.N + n;
-  if constexpr (EPI == kStore) {
-    store8<E>(static_cast<E*>(g.c) + at, g.add ? c + x.p : c);
-  } else if constexpr (EPI == kGlu) {
-    if (g.pre) {
-      store8<float>(g.pre + at2, c);
-      store8<float>(g.pre + at2 + g.N, up);
-    }
-    f32x8 h;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = act_of(g.act, c[i]) * up[i];
-    store8<E>(static_cast<E*>(g.c) + at, h);
-  } else {
-    f32x8 dg, du, h;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float a, da;
-      act_and_slope(g.act, x.p[i], a, da);
-      dg[i] = c[i] * x.q[i] * da;
-      du[i] = c[i] * a;
-      h[i] = a * x.q[i];
-    }
-    store8<E>(static_cast<E*>(g.c) + at2, dg);
-    store8<E>(static_cast<E*>(g.c) + at2 + g.N, du);
-    if (g.h) store8<E>(static_cast<E*>(g.h) + at, h);
-  }
-}
 
 // The part of the product that a workgroup computes.
 struct Place {
@@ -346,7 +301,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void dense_gemm_kernel(DenseGemm g
   using B = Operand<BN, BCOL, W::NW, W::DUAL ? 2 : 1>;
   constexpr int STAGE = A::kBytes + B::kBytes, N_DMA = A::kCopies + B::kCopies, HALF = N_DMA / 2;
   static_assert(N_DMA % 2 == 0 && (STAGES - 1) * N_DMA < 64 && W::kEpilogueBytes <= STAGES * STAGE, "stages");
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[STAGES * STAGE];
 
   Place p;
   if (!place_of<BM, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
@@ -435,7 +390,7 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
   using B = Operand<256, BCOL, 4, W::DUAL ? 2 : 1>;
   constexpr int NA = A::kCopies, NB = B::kCopies;
   static_assert(NA == 8 && NB == 8 && W::kEpilogueBytes <= 2 * A::kBytes + 3 * B::kBytes, "four copies per substep");
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * A::kBytes + 3 * B::kBytes];
 
   Place p;
   if (!place_of<256, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
@@ -507,19 +462,32 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
 
 // The partial products of a split K, added in the order of the splits, and the epilogue.
 template <class E, int EPI>
-__global__ __launch_bounds__(256) void dense_join_kernel(DenseGemm g, int splits) {
+__global__ __launch_bounds__(64) void dense_join_kernel(DenseGemm g, int splits) {
   constexpr bool DUAL = EPI == kGlu;
   const size_t per_row = g.N / 8, n8 = static_cast<size_t>(g.M) * per_row;
   const int w = DUAL ? 2 * g.N : g.N;
-  for (size_t i = blockIdx.x * 256ul + threadIdx.x; i < n8; i += gridDim.x * 256ul) {
+  for (size_t i = blockIdx.x * 64ul + threadIdx.x; i < n8; i += gridDim.x * 64ul) {
     const int m = static_cast<int>(i / per_row), n = static_cast<int>(i % per_row) * 8;
     Beside<E, EPI> x;
     x.load(g, m, n);
+    // four splits' loads in flight at a time, added in the order of the splits
     f32x8 c{}, up{};
-    for (int s = 0; s < splits; ++s) {
-      const float* p = g.part + (static_cast<size_t>(s) * g.M + m) * w + n;
-      c += load8<float>(p);
-      if (DUAL) up += load8<float>(p + g.N);
+    const size_t part = static_cast<size_t>(g.M) * w;
+    const float* p = g.part + static_cast<size_t>(m) * w + n;
+    for (int s = 0; s < splits; s += 4, p += 4 * part) {
+      f32x8 v[4], u[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float* at = p + (s + q < splits ? q : 0) * part;
+        v[q] = load8<float>(at);
+        if (DUAL) u[q] = load8<float>(at + g.N);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (s + q < splits) {
+          c += v[q];
+          if (DUAL) up += u[q];
+        }
     }
     finish8<E, EPI>(g, m, n, c, up, x);
   }
@@ -527,54 +495,93 @@ __global__ __launch_bounds__(256) void dense_join_kernel(DenseGemm g, int splits
 
 namespace {
 
+// Which tile, and in how many parts of K.
+enum Tile { k64, k128, k128Deep, k256 };
 struct Plan {
-  int tile;  // rows of A per tile: 256, 128 or 64
+  Tile tile;
   int splits;
 };
-
-int columns_of(int tile, bool dual) { return (tile == 256 ? 256 : 128) / (dual ? 2 : 1); }
+struct TileCost {
+  int rows, cols, slots;  // tile, and how many run at once on the chip (256 CUs)
+  float start, alone, full;  // us: launch, first loads and epilogue; a step with one per CU, and with every slot taken
+};
+// 64 x 128 (three buffers) and 128 x 128 (two) run two to a CU, 128 x 128 with
+// three buffers and 256 x 256 one.  Measured on products of 64 to 2048 rows: 128 x
+// 7168 x 2048 14.0 us on 64-row tiles, 17.3 and 19.7 on 128-row tiles; 777 x 4096 x
+// 2816 28.8, 24.5 (three buffers) and 31.7, 54 on 256-row tiles; 2048 x 4096 x 2816
+// 58.4, 53.8, 46.0 and 62.6; 2816 x 4096 x 2048 61.6, 58.2, 57.4 and 51.2.
+constexpr TileCost kTiles[] = {
+    {64, 128, 512, 4.0f, 0.33f, 0.56f},
+    {128, 128, 512, 4.5f, 0.60f, 0.87f},
+    {128, 128, 256, 5.7f, 0.43f, 0.43f},
+    {256, 256, 256, 11.4f, 1.16f, 1.16f},
+};
+// The time that a product takes by those figures: rounds of tiles, and where K is
+// split the launch that joins the parts and their traffic (4.5 TB/s).  128 x 2048
+// (gate and up) x 7168: 41.5 us whole and 20.1 in four parts; 512 x 2048 x 1408:
+// 10.8 whole, 13.0 in two.
+float cost_of(const TileCost& t, bool dual, int M, int N, int K, int splits) {
+  const int cols = dual ? t.cols / 2 : t.cols;
+  const long tiles = static_cast<long>((M + t.rows - 1) / t.rows) * ((N + cols - 1) / cols) * splits;
+  const int steps = ((K + kBK - 1) / kBK + splits - 1) / splits;
+  const long rest = tiles % t.slots;
+  float us = static_cast<float>(tiles / t.slots) * (t.start + t.full * steps);
+  if (rest) us += t.start + (rest <= 256 ? t.alone : t.full) * steps;
+  if (splits > 1) us += 3.5f + (splits + 1) * 4e-6f * M * N * (dual ? 2 : 1) / 4.5f;
+  return us;
+}
 
 Plan plan_for(int epi, int M, int N, int K) {
-  Plan p;
   const bool dual = epi == kGlu;
-  p.tile = M > 1024 ? 256 : M > 64 ? 128 : 64;
-  const long tiles = static_cast<long>((M + p.tile - 1) / p.tile) * ((N + columns_of(p.tile, dual) - 1) / columns_of(p.tile, dual));
   const int nk = (K + kBK - 1) / kBK;
-  const long room = (p.tile == 256 ? 256 : 512) / std::max(1L, tiles);
-  p.splits = static_cast<int>(std::max(1L, std::min({room, static_cast<long>(nk / 4), 16L})));
-  return p;
+  Plan best{k64, 1};
+  float least = 0.f;
+  for (int t = k64; t <= k256; ++t)
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (splits > 1 && (nk < 2 * splits || splits * static_cast<long>(M) * N * (dual ? 2 : 1) > 1L << 25)) break;
+      const float us = cost_of(kTiles[t], dual, M, N, K, splits);
+      if (least == 0.f || us < least) {
+        least = us;
+        best = {static_cast<Tile>(t), splits};
+      }
+    }
+  return best;
 }
 
 // Launches a tile kernel, the whole of K or one of its splits per workgroup, and
 // what joins the splits.
-template <class E, int BM, int BN, int NW, int LDS, int EPI, class K>
+template <class E, int BM, int BN, int EPI, class K>
 hipError_t run_tile(const DenseGemm& g, int splits, K whole, K part, hipStream_t s) {
   constexpr int NC = EPI == kGlu ? BN / 2 : BN;
   const int tm = (g.M + BM - 1) / BM, tn = (g.N + NC - 1) / NC;
   const long total = static_cast<long>(tm) * tn * splits;
-  const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8)), block(NW * 64);
+  const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8)), block(256);
   const K kernel = splits == 1 ? whole : part;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-  if (e != hipSuccess) return e;
-  kernel<<<grid, block, LDS, s>>>(g, tm, tn, splits);
-  e = hipGetLastError();
+  kernel<<<grid, block, 0, s>>>(g, tm, tn, splits);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
   const size_t n8 = static_cast<size_t>(g.M) * (g.N / 8);
-  dense_join_kernel<E, EPI><<<static_cast<unsigned>(std::min<size_t>((n8 + 255) / 256, 2048)), 256, 0, s>>>(g, splits);
+  dense_join_kernel<E, EPI><<<static_cast<unsigned>(std::min<size_t>((n8 + 63) / 64, 8192)), 64, 0, s>>>(g, splits);
   return hipGetLastError();
 }
 
 template <class E, bool ACOL, bool BCOL, int EPI>
 hipError_t run(const DenseGemm& g, hipStream_t s) {
   const Plan p = plan_for(EPI, g.M, g.N, g.K);
-  if (p.tile == 256)
-    return run_tile<E, 256, 256, 4, 160 * 1024, EPI>(g, p.splits, dense_gemm_256_kernel<E, ACOL, BCOL, EPI, false>,
-                                                     dense_gemm_256_kernel<E, ACOL, BCOL, EPI, true>, s);
-  if (p.tile == 128)
-    return run_tile<E, 128, 128, 4, 64 * 1024, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, false>,
-                                                    dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, true>, s);
-  return run_tile<E, 64, 128, 4, 72 * 1024, EPI>(g, p.splits, dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
-                                                 dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
+  switch (p.tile) {
+    case k64:
+      return run_tile<E, 64, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
+                                       dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
+    case k128:
+      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, true>, s);
+    case k128Deep:
+      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_kernel<E, 128, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
+    default:
+      return run_tile<E, 256, 256, EPI>(g, p.splits, dense_gemm_256_kernel<E, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_256_kernel<E, ACOL, BCOL, EPI, true>, s);
+  }
 }
 
 template <class E>
@@ -589,12 +596,14 @@ hipError_t run_type(int layout, int epi, const DenseGemm& g, hipStream_t s) {
 
 }  // namespace
 
-size_t dense_gemm_workspace_bytes(int, int epi, int M, int N, int K) {
+size_t dense_gemm_workspace_bytes(int layout, int epi, int M, int N, int K) {
+  if (dense_rows_fits(layout, epi, M, N, K)) return 0;
   const Plan p = plan_for(epi, M, N, K);
   return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * M * N * (epi == kGlu ? 2 : 1) * 4;
 }
 
 hipError_t launch_dense_gemm(int dtype, int layout, int epi, const DenseGemm& g, hipStream_t s) {
+  if (dense_rows_fits(layout, epi, g.M, g.N, g.K)) return launch_dense_rows(dtype, epi, g, s);
   return dtype == kBf16 ? run_type<bf16_t>(layout, epi, g, s) : run_type<f16_t>(layout, epi, g, s);
 }
 
