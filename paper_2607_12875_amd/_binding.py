@@ -6,7 +6,6 @@ fallback of any kind: a missing library or a non-OK status raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -315,22 +314,40 @@ def moe_forward(hidden, logits, w1, w2, top_k, *, mode="softmax", renormalize=Tr
 
 
 # ------------------------------------------------- norm, feed-forward block
-def _like(t, ref, name, shape=None, dtype=None):
-    """t is None, or a contiguous device tensor beside ref of that shape and type."""
-    if t is None:
-        return
-    if (not t.is_cuda or t.device != ref.device or not t.is_contiguous()
-            or t.shape != (ref.shape if shape is None else shape) or t.dtype != (ref.dtype if dtype is None else dtype)):
-        raise ValueError(f"{name}: expected a contiguous {dtype or ref.dtype} tensor of shape "
-                         f"{tuple(ref.shape if shape is None else shape)} on {ref.device}")
-
-
 def _rows(x, name):
-    if not x.is_cuda or not x.is_contiguous() or x.dim() != 2:
+    """Shape and device index of a contiguous [T, width] device tensor."""
+    i = x.get_device()
+    if i < 0 or x.dim() != 2 or not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous two-dimensional device tensor")
-    if x.dtype not in DTYPE:
+    return x.shape, i
+
+
+def _dtype(x, name):
+    d = DTYPE.get(x.dtype)
+    if d is None:
         raise ValueError(f"{name}: {x.dtype} is not supported")
-    return x.shape
+    return d
+
+
+def _at(t, name, shape, dtype, index):
+    """The address of t: None, or a contiguous tensor of that shape and type on device `index`."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}")
+    return t.data_ptr()
+
+
+def _call(f, where, index, stream, *args):
+    """f(*args, stream) on device `index`, on its current stream if none is given."""
+    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        status = f(*args, s)
+    else:
+        with torch.cuda.device(index):
+            status = f(*args, s)
+    if status != MOE_OK:
+        raise MoeError(status, where)
 
 
 def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1e-5, y=None, sum_out=None,
@@ -341,27 +358,25 @@ def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1
     s is what was normalised: x itself, or the sum rounded to the type (in
     sum_out where given).  mean and rstd (fp32 [T], for moe_norm_backward) are
     None without stats, mean also for "rms".  weight and bias [H] in x's type."""
-    T, H = _rows(x, "x")
-    _like(weight, x, "weight", (H,))
-    _like(bias, x, "bias", (H,))
-    _like(residual, x, "residual")
-    _like(y, x, "y")
-    _like(sum_out, x, "sum_out")
+    shape, i = _rows(x, "x")
+    T, H = shape
+    dt, dtype = x.dtype, _dtype(x, "x")
+    pw, pb = _at(weight, "weight", (H,), dt, i), _at(bias, "bias", (H,), dt, i)
+    pr = _at(residual, "residual", shape, dt, i)
     if y is None:
         y = torch.empty_like(x)
     if residual is None:
         sum_out = None
     elif sum_out is None:
         sum_out = torch.empty_like(x)
+    py, ps = _at(y, "y", shape, dt, i), _at(sum_out, "sum_out", shape, dt, i)
     mean = rstd = None
     if stats:
         rstd = torch.empty(T, dtype=torch.float32, device=x.device)
         if kind != "rms":
             mean = torch.empty_like(rstd)
-    with _on(x):
-        _check(lib().moe_norm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), T, H, NORM[kind],
-                                      DTYPE[x.dtype], float(eps), _ptr(y), _ptr(sum_out), _ptr(mean), _ptr(rstd),
-                                      _stream_of(x, stream)), "moe_norm_forward")
+    _call(lib().moe_norm_forward, "moe_norm_forward", i, stream, x.data_ptr(), pr, pw, pb, T, H, NORM[kind], dtype,
+          eps, py, ps, _ptr(mean), _ptr(rstd))
     return y, x if residual is None else sum_out, mean, rstd
 
 
@@ -374,26 +389,20 @@ def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=
     (mean None for "rms"); dsum (or None) the gradient that reaches s on its
     other way, added to dx.  workspace: a uint8 tensor of
     moe_norm_backward_workspace_bytes, or None to allocate one."""
-    T, H = _rows(x, "x")
-    _like(dy, x, "dy")
-    _like(weight, x, "weight", (H,))
-    _like(mean, x, "mean", (T,), torch.float32)
-    _like(rstd, x, "rstd", (T,), torch.float32)
-    _like(dsum, x, "dsum")
-    _like(dx, x, "dx")
+    shape, i = _rows(x, "x")
+    T, H = shape
+    dt, dtype, f32 = x.dtype, _dtype(x, "x"), torch.float32
+    pdy, pw, pds = _at(dy, "dy", shape, dt, i), _at(weight, "weight", (H,), dt, i), _at(dsum, "dsum", shape, dt, i)
+    pm, prs = _at(mean, "mean", (T,), f32, i), _at(rstd, "rstd", (T,), f32, i)
     if dx is None:
         dx = torch.empty_like(x)
-    dweight = torch.empty(H, dtype=torch.float32, device=x.device) if need_dweight else None
-    dbias = torch.empty(H, dtype=torch.float32, device=x.device) if need_dbias else None
-    nws = 0
-    if need_dweight or need_dbias:
-        nws = lib().moe_norm_backward_workspace_bytes(T, H)
-        workspace = _workspace(workspace, nws, x)
-    with _on(x):
-        _check(lib().moe_norm_backward(_ptr(dy), _ptr(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dsum), T, H,
-                                       NORM[kind], DTYPE[x.dtype], _ptr(dx), _ptr(dweight), _ptr(dbias),
-                                       _ptr(workspace) if nws else None, nws, _stream_of(x, stream)),
-               "moe_norm_backward")
+    pdx = _at(dx, "dx", shape, dt, i)
+    dweight = torch.empty(H, dtype=f32, device=x.device) if need_dweight else None
+    dbias = torch.empty(H, dtype=f32, device=x.device) if need_dbias else None
+    nws = lib().moe_norm_backward_workspace_bytes(T, H) if need_dweight or need_dbias else 0
+    workspace = _workspace(workspace, nws, x) if nws else None
+    _call(lib().moe_norm_backward, "moe_norm_backward", i, stream, pdy, x.data_ptr(), pw, pm, prs, pds, T, H,
+          NORM[kind], dtype, pdx, _ptr(dweight), _ptr(dbias), _ptr(workspace), nws)
     return dx, dweight, dbias
 
 
@@ -403,21 +412,11 @@ def moe_norm_backward_workspace_bytes(T: int, H: int) -> int:
 
 def _workspace(ws, need, ref):
     """ws if it holds need bytes on ref's device, else a new one."""
-    if ws is None or ws.numel() * ws.element_size() < need or ws.device != ref.device:
+    if ws is None or ws.numel() * ws.element_size() < need or ws.get_device() != ref.get_device():
         return torch.empty(max(need, 256), dtype=torch.uint8, device=ref.device)
     if not ws.is_contiguous():
         raise ValueError("workspace: expected a contiguous tensor")
     return ws
-
-
-def _on(ref):
-    """The context of ref's device, where that is not the current one."""
-    return contextlib.nullcontext() if ref.device.index == torch.cuda.current_device() else torch.cuda.device(ref.device)
-
-
-def _stream_of(ref, stream):
-    s = torch.cuda.current_stream(ref.device) if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
 
 
 def make_ffn_args(T, H, I, *, dtype=torch.bfloat16, act="silu", x=None, w1=None, w2=None, add=None, y=None, pre=None,
@@ -434,14 +433,6 @@ def moe_ffn_backward_workspace_bytes(args: MoeFfnArgs) -> int:
     return lib().moe_ffn_backward_workspace_bytes(ctypes.byref(args))
 
 
-def _ffn_shapes(x, w1, w2):
-    T, H = _rows(x, "x")
-    I = w2.shape[-1]
-    _like(w1, x, "w1", (2 * I, H))
-    _like(w2, x, "w2", (H, I))
-    return T, H, I
-
-
 def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=None, workspace=None, stream=None):
     """Gated feed-forward block y = (act(x w1[:I]^T) * (x w1[I:]^T)) w2^T + add on
     bf16 or fp16 x [T,H], w1 [2I,H], w2 [H,I] (H and I multiples of 8): returns
@@ -449,19 +440,20 @@ def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=
 
     With save, pre (fp32 [T,2I]) keeps both projections for moe_ffn_backward,
     else it is None.  add [T,H] may be y itself."""
-    T, H, I = _ffn_shapes(x, w1, w2)
-    _like(add, x, "add")
-    _like(y, x, "y")
-    _like(pre, x, "pre", (T, 2 * I), torch.float32)
+    shape, i = _rows(x, "x")
+    T, H = shape
+    I, dt = w2.shape[-1], x.dtype
     if y is None:
         y = torch.empty_like(x)
     if save and pre is None:
         pre = torch.empty((T, 2 * I), dtype=torch.float32, device=x.device)
-    args = make_ffn_args(T, H, I, dtype=x.dtype, act=act, x=x, w1=w1, w2=w2, add=add, y=y, pre=pre)
-    workspace = _workspace(workspace, moe_ffn_workspace_bytes(args), x)
-    with _on(x):
-        _check(lib().moe_ffn_forward(ctypes.byref(args), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                     _stream_of(x, stream)), "moe_ffn_forward")
+    args = MoeFfnArgs(T, H, I, _dtype(x, "x"), ACT[act], x.data_ptr(), _at(w1, "w1", (2 * I, H), dt, i),
+                      _at(w2, "w2", (H, I), dt, i), _at(add, "add", shape, dt, i), _at(y, "y", shape, dt, i),
+                      _at(pre, "pre", (T, 2 * I), torch.float32, i))
+    at = ctypes.byref(args)
+    workspace = _workspace(workspace, lib().moe_ffn_workspace_bytes(at), x)
+    _call(lib().moe_ffn_forward, "moe_ffn_forward", i, stream, at, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
     return y, pre, workspace
 
 
@@ -470,20 +462,20 @@ def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=N
     """Backward pass of moe_ffn_forward from its pre: returns (dx, dw1, dw2,
     workspace), the gradients in x's type.  need says which of them are
     computed; the others are None."""
-    T, H, I = _ffn_shapes(x, w1, w2)
-    _like(dy, x, "dy")
-    _like(pre, x, "pre", (T, 2 * I), torch.float32)
-    _like(dx, x, "dx")
-    _like(dw1, x, "dw1", (2 * I, H))
-    _like(dw2, x, "dw2", (H, I))
+    shape, i = _rows(x, "x")
+    T, H = shape
+    I, dt = w2.shape[-1], x.dtype
     dx = None if not need[0] else torch.empty_like(x) if dx is None else dx
     dw1 = None if not need[1] else torch.empty_like(w1) if dw1 is None else dw1
     dw2 = None if not need[2] else torch.empty_like(w2) if dw2 is None else dw2
-    args = make_ffn_args(T, H, I, dtype=x.dtype, act=act, x=x, w1=w1, w2=w2, pre=pre, dy=dy, dx=dx, dw1=dw1, dw2=dw2)
-    workspace = _workspace(workspace, moe_ffn_backward_workspace_bytes(args), x)
-    with _on(x):
-        _check(lib().moe_ffn_backward(ctypes.byref(args), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                      _stream_of(x, stream)), "moe_ffn_backward")
+    args = MoeFfnArgs(T, H, I, _dtype(x, "x"), ACT[act], x.data_ptr(), _at(w1, "w1", (2 * I, H), dt, i),
+                      _at(w2, "w2", (H, I), dt, i), None, None, _at(pre, "pre", (T, 2 * I), torch.float32, i),
+                      _at(dy, "dy", shape, dt, i), _at(dx, "dx", shape, dt, i), _at(dw1, "dw1", (2 * I, H), dt, i),
+                      _at(dw2, "dw2", (H, I), dt, i))
+    at = ctypes.byref(args)
+    workspace = _workspace(workspace, lib().moe_ffn_backward_workspace_bytes(at), x)
+    _call(lib().moe_ffn_backward, "moe_ffn_backward", i, stream, at, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
     return dx, dw1, dw2, workspace
 
 

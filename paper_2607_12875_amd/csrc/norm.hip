@@ -19,6 +19,7 @@ namespace moe {
 
 namespace {
 
+constexpr int kMostLds = 158 * 1024;  // column sums in LDS, beside 256 bytes of its own
 constexpr int kNormBlocks = 256;  // workgroups of the backward pass at most: one per CU
 
 template <class E> struct Chunk {
@@ -33,6 +34,14 @@ template <class E> struct Chunk {
 #pragma unroll
       for (int e = 0; e < W; ++e) f[e] = c * W + e < H ? static_cast<float>(row[c * W + e]) : 0.f;
     }
+  }
+  __device__ static u32x4 raw(const E* row, int c, int H) {
+    if (c * W + W <= H) return reinterpret_cast<const Bits*>(row + c * W)->v;
+    typedef E V __attribute__((ext_vector_type(W)));
+    V v;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[e] = c * W + e < H ? row[c * W + e] : static_cast<E>(0.f);
+    return __builtin_bit_cast(u32x4, v);
   }
   __device__ static void store(E* row, int c, int H, const float (&f)[W]) {
     if (c * W + W <= H) {
@@ -58,21 +67,29 @@ template <class E> struct Chunk {
   }
 };
 
+// Sum over the wave: four DPP permutes inside each row of sixteen lanes, then the
+// four rows' sums as scalars.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  v = dpp_add<0xB1>(v);   // quad_perm 1 0 3 2
+  v = dpp_add<0x4E>(v);   // quad_perm 2 3 0 1
+  v = dpp_add<0x141>(v);  // row_half_mirror
+  v = dpp_add<0x140>(v);  // row_mirror
+  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
 }
 
-// Sums of N values over the G threads of a row group (G a power of two, at least a
-// wave); `slots` holds N floats per wave of the workgroup.  Groups of several waves
-// meet in LDS, added in wave order, so every thread has the same sums.
+// Sums of N values over the G threads of a row group (one to sixteen waves);
+// `slots` holds N floats per wave of the workgroup.  Groups of several waves meet in
+// LDS: a lane per wave reads its sum, and the row of sixteen lanes adds them.
 template <int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], int G, float* slots) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
   if (G == kWave) return;
-  const int wave = threadIdx.x / kWave, nw = G / kWave, first = wave / nw * nw;
+  const int wave = threadIdx.x / kWave, nw = G / kWave, first = wave / nw * nw, l = lane_id() & 15;
   if (lane_id() == 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) slots[wave * N + i] = v[i];
@@ -80,8 +97,8 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int G, float* slots) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    v[i] = 0.f;
-    for (int w = 0; w < nw; ++w) v[i] += slots[(first + w) * N + i];
+    const float s = l < nw ? slots[(first + l) * N + i] : 0.f;
+    v[i] = dpp_add<0x140>(dpp_add<0x141>(dpp_add<0x4E>(dpp_add<0xB1>(s))));
   }
 }
 
@@ -149,134 +166,229 @@ __global__ __launch_bounds__(1024) void norm_forward_kernel(NormForward a, int G
   }
 }
 
+// Four columns of a row of sums from column h on (16-byte aligned), up to `end`.
+__device__ __forceinline__ void put4(float* row, int h, int end, const f32x4& v) {
+  if (!row) return;
+  if (h + 4 <= end) {
+    *reinterpret_cast<f32x4*>(row + h) = v;
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (h + q < end) row[h + q] = v[q];
+  }
+}
+
 // Each workgroup takes every gridDim-th set of rows, its row groups one each, and
 // keeps its columns' sums of dy xhat and dy in registers; at the end the groups'
-// sums are joined in LDS, in order, and written as one row of partial sums.
-template <class E, int NV, int KIND>
+// sums are joined in LDS, in order, and written as one row of partial sums.  The
+// next rows are in flight, unconverted, while a row is reduced and written: without,
+// the barrier of every row stood between the loads (8192 x 4096 bf16 with dsum, 268
+// MB: 102 us; 46 now).  Rows so wide that a thread has several chunks keep
+// the column sums in LDS (IN_LDS; each thread its own columns, so without atomics),
+// where they fit: in registers they would spill.
+template <class E, int NV, int KIND, bool IN_LDS>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackward a, int G) {
   using C = Chunk<E>;
+  constexpr int W = C::W, NR = IN_LDS ? 1 : NV;
   __shared__ float slots[2][2 * 16];
-  extern __shared__ float joined[];  // [2][H] with more than one row group
-  const int groups = blockDim.x / G, gi = threadIdx.x / G, gt = threadIdx.x % G;
-  float dw[NV][C::W], db[NV][C::W], w[NV][C::W];
+  extern __shared__ __attribute__((aligned(16))) float joined[];  // IN_LDS: [2][H up to whole chunks], the sums; else the row groups' sums at the end
+  const int groups = blockDim.x / G, gi = threadIdx.x / G, gt = threadIdx.x % G, Hp = (a.H + 7) / 8 * 8;
+  float dw[NR][W], db[NR][W];
+  u32x4 w[NV], x1[NV], g1[NV], d1[NV];  // weight; the next row's x, dy, dsum
+  float mean1 = 0.f, rstd1 = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    C::load(static_cast<const E*>(a.weight), gt + i * G, a.H, w[i]);
+    w[i] = C::raw(static_cast<const E*>(a.weight), gt + i * G, a.H);
 #pragma unroll
-    for (int e = 0; e < C::W; ++e) dw[i][e] = db[i][e] = 0.f;
+    for (int e = 0; e < W; ++e) {
+      const int h = (gt + i * G) * W + e;
+      if constexpr (!IN_LDS) dw[i][e] = db[i][e] = 0.f;
+      else if (h < Hp) joined[h] = joined[Hp + h] = 0.f;
+    }
   }
-  const float inv = 1.0f / a.H;
-  int turn = 0;
-  for (int r0 = blockIdx.x * groups; r0 < a.T; r0 += gridDim.x * groups, turn ^= 1) {
-    const int row = r0 + gi;
-    const bool live = row < a.T;
-    const size_t at = static_cast<size_t>(live ? row : r0) * a.H;
-    float x[NV][C::W], g[NV][C::W];
-    const float rstd = a.rstd[live ? row : r0], mean = KIND == kLayerNorm ? a.mean[live ? row : r0] : 0.f;
+  auto fetch = [&](int r0) {
+    const int row = min(r0 + gi, a.T - 1);
+    const size_t at = static_cast<size_t>(row) * a.H;
+    rstd1 = a.rstd[row];
+    if (KIND == kLayerNorm) mean1 = a.mean[row];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      C::load(static_cast<const E*>(a.x) + at, gt + i * G, a.H, x[i]);
-      C::load(static_cast<const E*>(a.dy) + at, gt + i * G, a.H, g[i]);
+      x1[i] = C::raw(static_cast<const E*>(a.x) + at, gt + i * G, a.H);
+      g1[i] = C::raw(static_cast<const E*>(a.dy) + at, gt + i * G, a.H);
     }
+  };
+  auto fetch_dsum = [&](int r0) {
+    const size_t at = static_cast<size_t>(min(r0 + gi, a.T - 1)) * a.H;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) d1[i] = C::raw(static_cast<const E*>(a.dsum) + at, gt + i * G, a.H);
+  };
+  const float inv = 1.0f / a.H;
+  const int stride = gridDim.x * groups;
+  int turn = 0;
+  fetch(blockIdx.x * groups);
+  if (a.dsum) fetch_dsum(blockIdx.x * groups);
+  for (int r0 = blockIdx.x * groups; r0 < a.T; r0 += stride, turn ^= 1) {
+    const bool live = r0 + gi < a.T;
+    const size_t at = static_cast<size_t>(r0 + gi) * a.H;
+    const float rstd = rstd1, mean = mean1;
+    float x[NV][W], g[NV][W];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      C::unpack(x1[i], x[i]);
+      C::unpack(g1[i], g[i]);
+    }
+    if (r0 + stride < a.T) fetch(r0 + stride);
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      float wf[W];
+      C::unpack(w[i], wf);
+      float* const sw = joined + (gt + i * G) * W;
+      const bool mine = (gt + i * G) * W < a.H;
 #pragma unroll
-      for (int e = 0; e < C::W; ++e) {
-        x[i][e] = (x[i][e] - mean) * rstd;
-        if (live) {
+      for (int e = 0; e < W; ++e) x[i][e] = (x[i][e] - mean) * rstd;
+      if constexpr (IN_LDS) {
+        if (mine) {
+#pragma unroll
+          for (int e = 0; e < W; e += 4) {
+            f32x4 vw = *reinterpret_cast<f32x4*>(sw + e), vb = *reinterpret_cast<f32x4*>(sw + Hp + e);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              vw[q] = fmaf(g[i][e + q], x[i][e + q], vw[q]);
+              vb[q] += g[i][e + q];
+            }
+            *reinterpret_cast<f32x4*>(sw + e) = vw;
+            *reinterpret_cast<f32x4*>(sw + Hp + e) = vb;
+          }
+        }
+      } else if (live) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
           dw[i][e] = fmaf(g[i][e], x[i][e], dw[i][e]);
           db[i][e] += g[i][e];
         }
-        g[i][e] *= w[i][e];
+      }
+#pragma unroll
+      for (int e = 0; e < W; ++e) {
+        g[i][e] *= wf[e];
         sum[0] += g[i][e];
         sum[1] = fmaf(g[i][e], x[i][e], sum[1]);
       }
+    }
     group_sum(sum, G, slots[turn]);
-    if (!live) continue;
-    const float s1 = KIND == kLayerNorm ? sum[0] * inv : 0.f, s2 = sum[1] * inv;
+    if (live) {
+      const float s1 = KIND == kLayerNorm ? sum[0] * inv : 0.f, s2 = sum[1] * inv;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = gt + i * G;
-      if (c * C::W >= a.H) continue;
-      float d[C::W] = {};
-      if (a.dsum) C::load(static_cast<const E*>(a.dsum) + at, c, a.H, d);
+      for (int i = 0; i < NV; ++i) {
+        const int c = gt + i * G;
+        if (c * W >= a.H) continue;
+        float d[W] = {};
+        if (a.dsum) C::unpack(d1[i], d);
 #pragma unroll
-      for (int e = 0; e < C::W; ++e) d[e] = fmaf(rstd, g[i][e] - s1 - x[i][e] * s2, d[e]);
-      C::store(static_cast<E*>(a.dx) + at, c, a.H, d);
-    }
-  }
-  if (!a.part) return;
-  for (int q = groups - 1; q > 0; --q) {  // group 0 ends with the sums of all
-    if (gi == q) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < C::W; ++e) {
-          const int h = (gt + i * G) * C::W + e;
-          if (h < a.H) {
-            if (q < groups - 1) {
-              joined[h] += dw[i][e];
-              joined[a.H + h] += db[i][e];
-            } else {
-              joined[h] = dw[i][e];
-              joined[a.H + h] = db[i][e];
-            }
-          }
-        }
-    }
-    __syncthreads();
-  }
-  if (gi) return;
-  float* part = a.part + static_cast<size_t>(blockIdx.x) * 2 * a.H;
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < C::W; ++e) {
-      const int h = (gt + i * G) * C::W + e;
-      if (h < a.H) {
-        part[h] = dw[i][e] + (groups > 1 ? joined[h] : 0.f);
-        part[a.H + h] = db[i][e] + (groups > 1 ? joined[a.H + h] : 0.f);
+        for (int e = 0; e < W; ++e) d[e] = fmaf(rstd, g[i][e] - s1 - x[i][e] * s2, d[e]);
+        C::store(static_cast<E*>(a.dx) + at, c, a.H, d);
       }
     }
-}
-
-// Column sums of the partial rows: 64 columns per workgroup, sixteen slices of the rows.
-__global__ __launch_bounds__(1024) void norm_columns_kernel(const float* part, int rows, int H, float* dweight, float* dbias) {
-  __shared__ float s[16][kWave];
-  float* out = blockIdx.y ? dbias : dweight;
-  if (!out) return;
-  const int l = threadIdx.x % kWave, q = threadIdx.x / kWave, h = blockIdx.x * kWave + l;
-  float v = 0.f;
-  if (h < H)
-    for (int r = q; r < rows; r += 16) v += part[(static_cast<size_t>(r) * 2 + blockIdx.y) * H + h];
-  s[q][l] = v;
-  __syncthreads();
-  if (q == 0 && h < H) {
+    if (a.dsum && r0 + stride < a.T) fetch_dsum(r0 + stride);
+  }
+  if (!a.dweight && !a.dbias) return;
+  // with one workgroup its sums are the results, else a row of partial sums
+  float* const pw = gridDim.x == 1 ? a.dweight : a.part + static_cast<size_t>(blockIdx.x) * 2 * Hp;
+  float* const pb = gridDim.x == 1 ? a.dbias : pw + Hp;
+  if (!IN_LDS && groups > 1) {  // [group][2][G W]: every group's sums meet, in the order of the groups
+    const int width = G * W;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v += s[i][l];
-    out[h] = v;
+    for (int e = 0; e < W; ++e) {
+      joined[gi * 2 * width + gt * W + e] = dw[0][e];
+      joined[(gi * 2 + 1) * width + gt * W + e] = db[0][e];
+    }
+    __syncthreads();
+    for (int h = threadIdx.x; h < a.H; h += blockDim.x) {
+      float sw = joined[h], sb = joined[width + h];
+      for (int q = 1; q < groups; ++q) {
+        sw += joined[q * 2 * width + h];
+        sb += joined[(q * 2 + 1) * width + h];
+      }
+      if (pw) pw[h] = sw;
+      if (pb) pb[h] = sb;
+    }
+    return;
+  }
+  const int end = gridDim.x == 1 ? a.H : Hp;  // partial rows are whole chunks
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int h = (gt + i * G) * W;
+    if (h >= a.H) continue;
+#pragma unroll
+    for (int e = 0; e < W; e += 4) {
+      f32x4 vw, vb;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        vw[q] = IN_LDS ? joined[h + e + q] : dw[IN_LDS ? 0 : i][e + q];
+        vb[q] = IN_LDS ? joined[Hp + h + e + q] : db[IN_LDS ? 0 : i][e + q];
+      }
+      put4(pw, h + e, end, vw);
+      put4(pb, h + e, end, vb);
+    }
   }
 }
 
-// Threads per row and chunks per thread: H / W chunks over a power of two of
-// threads.
+// Column sums of the partial rows: 64 columns per workgroup, four per thread, 64
+// slices of the rows.
+__global__ __launch_bounds__(1024) void norm_columns_kernel(const float* part, int rows, int H, float* dweight, float* dbias) {
+  __shared__ f32x4 s[64][16];
+  float* out = blockIdx.y ? dbias : dweight;
+  if (!out) return;
+  const int l = threadIdx.x % 16, q = threadIdx.x / 16, h = (blockIdx.x * 16 + l) * 4, Hp = (H + 7) / 8 * 8;
+  f32x4 v{};
+  if (h < H)
+#pragma unroll 4
+    for (int r = q; r < rows; r += 64) v += *reinterpret_cast<const f32x4*>(part + (static_cast<size_t>(r) * 2 + blockIdx.y) * Hp + h);
+  s[q][l] = v;
+  __syncthreads();
+  if (q >= 4) return;
+  // four waves' worth of column groups: 16 slices each, then the four
+  for (int i = 1; i < 16; ++i) v += s[q + 4 * i][l];
+  s[q][l] = v;
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);  // one wave: its reads follow its writes
+  __builtin_amdgcn_wave_barrier();
+  if (q == 0 && h < H) {
+    v = (v + s[1][l]) + (s[2][l] + s[3][l]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (h + e < H) out[h + e] = v[e];
+  }
+}
+
+__global__ void norm_zero_kernel(float* a, float* b, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n && a) a[i] = 0.f;
+  if (i < n && b) b[i] = 0.f;
+}
+
+// Threads per row (whole waves) and chunks per thread, at most `most` of them
+// where 1024 threads can have the row.
 struct Shape {
   int G, NV;
 };
 Shape shape_of(int H, int width, int most) {
   const int chunks = (H + width - 1) / width;
-  Shape s{kWave, 1};
-  while (s.G < 1024 && s.G * most < chunks) s.G *= 2;
+  Shape s{std::min(1024, ((chunks + most - 1) / most + kWave - 1) / kWave * kWave), 1};
   while (s.G * s.NV < chunks) s.NV *= 2;
   return s;
 }
 
-int backward_threads(const Shape& s) { return std::max(s.G, 512); }
-int backward_blocks(int T, int groups) { return std::min(kNormBlocks, (T + groups - 1) / groups); }
+// Up to two rows per row group one workgroup does all, in one launch.
+// Otherwise each takes the same number of rows, or one less.
+// More workgroups than CUs write more partial sums than they save (777 x 5120: 14.3
+// us, with two per CU 16.5).
+int backward_blocks(int T, int groups) {
+  if (T <= 2 * groups) return 1;
+  const int sets = (T + groups - 1) / groups, each = (sets + kNormBlocks - 1) / kNormBlocks;
+  return (sets + each - 1) / each;
+}
 
-template <class E, int KIND, class F>
-hipError_t with_nv(int nv, F f) {
+template <class F> hipError_t with_nv(int nv, F f) {
   switch (nv) {
     case 1: return f(std::integral_constant<int, 1>{});
     case 2: return f(std::integral_constant<int, 2>{});
@@ -288,9 +400,11 @@ hipError_t with_nv(int nv, F f) {
 
 template <class E, int KIND>
 hipError_t forward(const NormForward& a, hipStream_t s) {
-  const Shape p = shape_of(a.H, Chunk<E>::W, a.T >= 1024 ? 4 : 1);
-  const int threads = std::max(256, p.G), rows = threads / p.G;
-  return with_nv<E, KIND>(p.NV, [&](auto nv) {
+  // few rows: as many threads as a row can use; many: two chunks each (8192 x 7168
+  // bf16 with residual 86 us, with four 92, 777 x 5120 7.2, with one 9.0)
+  const Shape p = shape_of(a.H, Chunk<E>::W, a.T >= 512 ? 2 : 1);
+  const int rows = std::max(1, 256 / p.G), threads = rows * p.G;
+  return with_nv(p.NV, [&](auto nv) {
     norm_forward_kernel<E, decltype(nv)::value, KIND><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a, p.G);
     return hipGetLastError();
   });
@@ -298,25 +412,38 @@ hipError_t forward(const NormForward& a, hipStream_t s) {
 
 template <class E, int KIND>
 hipError_t backward(const NormBackward& a, hipStream_t s) {
-  const Shape p = shape_of(a.H, Chunk<E>::W, 2);
-  const int threads = backward_threads(p), groups = threads / p.G, blocks = backward_blocks(a.T, groups);
-  const size_t lds = groups > 1 ? 2ul * a.H * 4 : 0;
+  const Shape p = shape_of(a.H, Chunk<E>::W, 1);
+  const int groups = p.NV > 1 ? 1 : 1024 / p.G, threads = groups * p.G, blocks = backward_blocks(a.T, groups);
+  const int sums = 2 * ((a.H + 7) / 8 * 8) * 4;
+  const bool in_lds = p.NV > 1 && sums <= kMostLds;
   if (a.T > 0) {
-    const hipError_t e = with_nv<E, KIND>(p.NV, [&](auto nv) {
-      norm_backward_kernel<E, decltype(nv)::value, KIND><<<blocks, threads, lds, s>>>(a, p.G);
+    const hipError_t e = with_nv(p.NV, [&](auto nv) {
+      constexpr int NV = decltype(nv)::value;
+      if constexpr (NV > 1) {
+        if (in_lds) {
+          const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(norm_backward_kernel<E, NV, KIND, true>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
+          if (e != hipSuccess) return e;
+          norm_backward_kernel<E, NV, KIND, true><<<blocks, threads, sums, s>>>(a, p.G);
+          return hipGetLastError();
+        }
+      }
+      // several row groups have one chunk per thread each
+      norm_backward_kernel<E, NV, KIND, false><<<blocks, threads, groups > 1 ? 2 * threads * Chunk<E>::W * 4 : 0, s>>>(a, p.G);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
   }
   if (!a.dweight && !a.dbias) return hipSuccess;
-  norm_columns_kernel<<<dim3((a.H + kWave - 1) / kWave, 2), 1024, 0, s>>>(a.part, blocks, a.H, a.dweight, a.dbias);
+  if (a.T == 0) norm_zero_kernel<<<(a.H + 255) / 256, 256, 0, s>>>(a.dweight, a.dbias, a.H);
+  else if (blocks > 1) norm_columns_kernel<<<dim3((a.H + 63) / 64, 2), 1024, 0, s>>>(a.part, blocks, a.H, a.dweight, a.dbias);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t norm_backward_workspace_bytes(int T, int H) {
-  return static_cast<size_t>(std::min(kNormBlocks, T)) * 2 * H * 4;
+  return static_cast<size_t>(std::min(kNormBlocks, T)) * 2 * ((H + 7) / 8 * 8) * 4;
 }
 
 hipError_t launch_norm_forward(int dtype, int kind, const NormForward& a, hipStream_t s) {
