@@ -22,13 +22,13 @@ namespace moe {
 constexpr int kBK = 64;  // K elements per step: 128 bytes, one line of a row operand
 
 // Sixteen bytes per lane from a bounds-checked buffer to LDS: lane l reads
-// offset voff and lands at lds + AT + 16 l.  Lanes past the buffer's end write
-// zeros.  The four wait states between the write of M0 and the copy (one is
-// needed for M0) also cover a descriptor word that the compiler took from a VGPR
-// just before.
+// offset voff + soff and lands at lds + AT + 16 l.  Lanes past the buffer's end
+// write zeros.  One wait state lies between the write of M0 and the copy; that the
+// descriptor's words are not written by a VALU operation in the five states before
+// is up to the caller, who makes them some products ahead.
 template <int AT>
-__device__ __forceinline__ void bdma16(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc), "i"(AT)
+__device__ __forceinline__ void bdma16(const u32x4& rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %4 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc), "i"(AT), "s"(soff)
                : "memory", "m0", "scc");
 }
 __device__ __forceinline__ u32x4 buffer_of(uint64_t base, uint32_t bytes) {
@@ -55,11 +55,14 @@ struct Operand {
   static_assert(!COL || (R >= 64 && PARTS == 1), "column tiles");
   __device__ static int tswz(int k) { return R == 64 ? (k & 2) << 1 : (k & 3) << 2; }
 
-  uint64_t base[PARTS];  // where the next step starts
-  int left[PARTS];       // row: bytes from there to the end of the tile's rows; column: bytes before it in its row
-  uint32_t voff[kCopies];
-  u32x4 desc[PARTS];     // the step being copied
-  uint32_t past;         // row: all ones above the offsets where the lane's chunk lies past K
+  // Row operand: the buffer is the tile's rows, whole, and a step's place in K an
+  // offset that all lanes share; rows past the last lie past the buffer's end, and
+  // in the last step of a ragged K the lanes past K are sent there.  Column operand:
+  // the buffer is the step's rows of K, so that those past K lie past its end.
+  u32x4 desc[PARTS];
+  uint32_t voff[kCopies], soff;
+  uint64_t base;          // column: where the next step starts
+  uint32_t whole, tail;   // column: bytes of a whole step's buffer and of a last, ragged one
   int ld, chunk;
 
   // The R rows (columns) from r0 on of an operand that has `count` of them, from
@@ -67,15 +70,15 @@ struct Operand {
   __device__ void start(const void* at, int r0, int count, int K, int k0, int apart) {
     const uint64_t first = reinterpret_cast<uint64_t>(at);
     ld = COL ? count : K;
+    soff = 0;
     if constexpr (COL) {
-      base[0] = first + (static_cast<uint64_t>(k0) * ld + r0) * 2;
-      left[0] = __builtin_amdgcn_readfirstlane(r0 * 2);
+      base = first + (static_cast<uint64_t>(k0) * ld + r0) * 2;
+      whole = (static_cast<uint32_t>(kBK) * ld - r0) * 2u;
+      tail = K % kBK ? (static_cast<uint32_t>(K % kBK) * ld - r0) * 2u : whole;
     } else {
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) {
-        base[p] = first + (static_cast<uint64_t>(r0 + p * apart) * ld + k0) * 2;
-        left[p] = __builtin_amdgcn_readfirstlane(max(0, max(0, min(count - r0, R / PARTS)) * ld * 2 - k0 * 2));
-      }
+      for (int p = 0; p < PARTS; ++p)
+        desc[p] = buffer_of(first + static_cast<uint64_t>(r0 + p * apart) * ld * 2, static_cast<uint32_t>(max(0, min(count - r0, R / PARTS))) * ld * 2u);
     }
   }
   __device__ void offsets(int wave, int lane) {
@@ -88,20 +91,23 @@ struct Operand {
     }
     static_assert(COL || NW % 2 == 0, "a lane's chunk is the same in every copy");
   }
-  // Make ready for the step that starts at k (of K; past its end the copies
-  // are zeros), and stand at the next one.
+  // Make ready for the step that starts at k (of K; past its end the copies are
+  // zeros).  Steps come in order.
   __device__ void step(int k, int K) {
+    if constexpr (COL) {
+      desc[0] = buffer_of(base, k + kBK <= K ? whole : k < K ? tail : 0u);
+      base += static_cast<uint64_t>(ld) * kBK * 2;
+    } else {
+      soff = k * 2u;
+      if (k + kBK > K) {  // uniform
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      desc[p] = buffer_of(base[p], COL ? max(0, max(0, min(K - k, kBK)) * ld * 2 - left[p]) : left[p]);
-      base[p] += COL ? static_cast<uint64_t>(ld) * kBK * 2 : kBK * 2;
-      if (!COL) left[p] = max(0, left[p] - kBK * 2);
+        for (int i = 0; i < kCopies; ++i) voff[i] = k + chunk * 8 >= K ? 0x80000000u : voff[i];
+      }
     }
-    if (!COL) past = k + chunk * 8 >= K ? 0x80000000u : 0u;
   }
   // Copy I of that step into LDS at `lds`, the buffer plus 1 KB per wave.
   template <int I> __device__ void copy(uint32_t lds) const {
-    bdma16<I * NW * 1024>(desc[I / (kCopies / PARTS)], COL ? voff[I] : voff[I] | past, lds);
+    bdma16<I * NW * 1024>(desc[I / (kCopies / PARTS)], voff[I], soff, lds);
   }
 
   // Fragments, eight consecutive k of group lane / 32 of a K substep for row
