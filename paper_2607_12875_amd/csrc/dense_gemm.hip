@@ -295,13 +295,14 @@ __device__ __forceinline__ void settle() {
   vm_wait<N>();
 }
 
-// Workgroup tile BM x BN (kGlu: BN / 2 gate and BN / 2 up rows of B) in WM x WN
-// waves; STAGES buffers of kBK.  Stage kt + STAGES goes into the buffer of stage
+// 128 x 128 tile (kGlu: 64 gate and 64 up rows of B), four waves of 64 x 64; STAGES
+// buffers of kBK.  Stage kt + STAGES goes into the buffer of stage
 // kt once every wave has read it (the barrier before the last substep of step
 // kt): half of its copies in that substep, half in the next.  Steps past the end
 // copy zeros, so there is no branch in the loop and every wait counts the same.
-template <class E, int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, int EPI, bool SPLIT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void dense_gemm_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+template <class E, int STAGES, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void dense_gemm_128_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+  constexpr int BM = 128, BN = 128, WM = 2, WN = 2;
   using W = Waves<BM, BN, WM, WN, EPI>;
   using A = Operand<BM, ACOL, W::NW, 1>;
   using B = Operand<BN, BCOL, W::NW, W::DUAL ? 2 : 1>;
@@ -377,6 +378,112 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void dense_gemm_kernel(DenseGemm g
   vm_wait<0>();
   bar();  // no wave reads the stages any more, no copy is under way
   epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
+}
+
+// 64 x 128 tile, four waves of 32 x 64, three buffers of kBK.  A wave's substep has
+// two products, 64 cycles, fewer than an LDS read takes, so the fragments of a whole
+// step are read during the step before (512 x 2048 x 1408: 8.8 us, one substep ahead
+// 10.8; 128 x 7168 x 2048 11.2 and 14.0).  A stage's buffer is free once every wave
+// has its fragments, at the barrier that opens its step, and stage kt + 3 goes there.
+template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void dense_gemm_64_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+  constexpr int BM = 64, BN = 128, WM = 2, WN = 2, STAGES = 3;
+  using W = Waves<BM, BN, WM, WN, EPI>;
+  using A = Operand<BM, ACOL, W::NW, 1>;
+  using B = Operand<BN, BCOL, W::NW, W::DUAL ? 2 : 1>;
+  constexpr int STAGE = A::kBytes + B::kBytes, N_DMA = A::kCopies + B::kCopies;
+  constexpr int TM = W::TM, TN = W::TN, R = TM + TN, NKK = kBK / 16, N = TM * TN * NKK;
+  static_assert((STAGES - 1) * N_DMA < 64 && W::kEpilogueBytes <= STAGES * STAGE, "stages");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[STAGES * STAGE];
+
+  Place p;
+  if (!place_of<BM, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  A a;
+  B b;
+  a.start(g.a, p.m0, g.M, g.K, p.k_first, 0);
+  b.start(g.b, p.n0, g.N, g.K, p.k_first, g.N);
+  a.offsets(wave, lane);
+  b.offsets(wave, lane);
+  auto ready = [&](int kt) {
+    a.step(p.k_first + kt * kBK, p.k_end);
+    b.step(p.k_first + kt * kBK, p.k_end);
+  };
+  const uint32_t smem0 = lds_addr(smem), mine = wave * 1024;
+  auto copy = [&](auto i, uint32_t buf) {
+    if constexpr (i < A::kCopies) a.template copy<i>(buf + mine);
+    else b.template copy<i - A::kCopies>(buf + A::kBytes + mine);
+  };
+  auto next = [&](uint32_t at) { return at + STAGE == smem0 + STAGES * STAGE ? smem0 : at + STAGE; };
+
+  u32x4 fa[2][NKK][TM], fb[2][NKK][TN];
+  f32x16 acc[TM][TN];
+  uint32_t la[4], lb[4], pa[4], pb[4];
+  A::lanes(la, wm * W::WTM, lane);
+  B::lanes(lb, W::bfirst(wn), lane);
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
+  auto from = [&](uint32_t at) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      pa[q] = la[q] + at;
+      pb[q] = lb[q] + at + A::kBytes;
+    }
+  };
+  // fragment f of a step, in the order that the products want them, into set s
+  auto read = [&](auto s, auto f) {
+    constexpr int kk = f / R, r = f % R;
+    if constexpr (r < TN) fb[s][kk][r] = B::frag(pb, r, W::brows(r), kk);
+    else fa[s][kk][r - TN] = A::frag(pa, r - TN, (r - TN) * 32, kk);
+  };
+  uint32_t rd = smem0;  // the buffer of stage kt
+  // One step: set s multiplied, the other read from stage kt + 1, stage kt + STAGES
+  // copied over stage kt, spread over the products.
+  auto step = [&](auto s, int kt) {
+    constexpr int WORK = NKK * R + N_DMA;
+    const uint32_t wr = rd;
+    rd = next(rd);
+    from(rd);
+    ready(kt + STAGES);
+    settle<(STAGES - 2) * N_DMA>();
+    bar();  // stage kt + 1 has landed, stage kt is in registers everywhere
+    each<N>([&](auto n) {
+      constexpr int kk = n / (TM * TN), i = n % (TM * TN) / TN, j = n % TN;
+      acc[i][j] = mfma32<E>(fb[s][kk][j], fa[s][kk][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      constexpr int w0 = n * WORK / N, w1 = (n + 1) * WORK / N;
+      each<w1 - w0>([&](auto w) {
+        constexpr int at = (w0 + w + NKK * R) % WORK;  // copies first
+        if constexpr (at < NKK * R) read(std::integral_constant<int, 1 - s>{}, std::integral_constant<int, at>{});
+        else copy(std::integral_constant<int, at - NKK * R>{}, wr);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  uint32_t wr = smem0;
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) {
+    ready(s);
+    each<N_DMA>([&](auto i) { copy(i, wr); });
+    wr = next(wr);
+  }
+  vm_wait<(STAGES - 1) * N_DMA>();
+  bar();
+  from(rd);
+  typedef std::integral_constant<int, 0> even;
+  typedef std::integral_constant<int, 1> odd;
+  each<NKK * R>([&](auto f) { read(even{}, f); });
+  for (int kt = 0; kt < p.nk; kt += 2) {
+    step(even{}, kt);
+    if (kt + 1 < p.nk) step(odd{}, kt + 1);
+  }
+  vm_wait<0>();
+  bar();  // no wave reads the stages any more, no copy is under way
+  epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, acc);
 }
 
 // 256 x 256 tile, four waves of 128 x 128, each with a SIMD to itself (the sums
@@ -512,20 +619,21 @@ struct TileCost {
   float start, alone, full;  // us: launch, first loads and epilogue; a step with one per CU, and with every slot taken
 };
 // 64 x 128 (three buffers) and 128 x 128 (two) run two to a CU, 128 x 128 with
-// three buffers and 256 x 256 one.  Measured on products of 64 to 2048 rows: 128 x
-// 7168 x 2048 14.0 us on 64-row tiles, 17.3 and 19.7 on 128-row tiles; 777 x 4096 x
-// 2816 28.8, 24.5 (three buffers) and 31.7, 54 on 256-row tiles; 2048 x 4096 x 2816
-// 58.4, 53.8, 46.0 and 62.6; 2816 x 4096 x 2048 61.6, 58.2, 57.4 and 51.2.
+// three buffers and 256 x 256 one.  Fitted to 400 timings of products of 40 to 2048
+// rows; what the figures choose takes 2 % more than the quickest on average, 15 % at
+// worst.  Among them, us, on 64-, 128-, 128- (three buffers) and 256-row tiles: 128 x
+// 7168 x 2048 11.4, 18.4, 15.3, -; 777 x 4096 x 2816 29.1, 31.3, 24.5, 54; 2048 x 4096
+// x 2816 60, 48, 54, 63; 2816 x 4096 x 2048 63, 57, 57, 52.
 constexpr TileCost kTiles[] = {
-    {64, 128, 512, 4.0f, 0.33f, 0.56f},
-    {128, 128, 512, 4.5f, 0.60f, 0.87f},
-    {128, 128, 256, 5.7f, 0.43f, 0.43f},
-    {256, 256, 256, 11.4f, 1.16f, 1.16f},
+    {64, 128, 512, 4.0f, 0.26f, 0.56f},
+    {128, 128, 512, 4.7f, 0.49f, 0.86f},
+    {128, 128, 256, 4.5f, 0.43f, 0.43f},
+    {256, 256, 256, 10.4f, 1.14f, 1.14f},
 };
 // The time that a product takes by those figures: rounds of tiles, and where K is
-// split the launch that joins the parts and their traffic (4.5 TB/s).  128 x 2048
-// (gate and up) x 7168: 41.5 us whole and 20.1 in four parts; 512 x 2048 x 1408:
-// 10.8 whole, 13.0 in two.
+// split the launch that joins the parts and their traffic.  128 x 2048 (gate and up)
+// x 7168: 33 us whole and 19.6 in three parts; 512 x 2048 x 1408: 8.9 whole, 12.4 in
+// two.
 float cost_of(const TileCost& t, bool dual, int M, int N, int K, int splits) {
   const int cols = dual ? t.cols / 2 : t.cols;
   const long tiles = static_cast<long>((M + t.rows - 1) / t.rows) * ((N + cols - 1) / cols) * splits;
@@ -533,7 +641,7 @@ float cost_of(const TileCost& t, bool dual, int M, int N, int K, int splits) {
   const long rest = tiles % t.slots;
   float us = static_cast<float>(tiles / t.slots) * (t.start + t.full * steps);
   if (rest) us += t.start + (rest <= 256 ? t.alone : t.full) * steps;
-  if (splits > 1) us += 3.5f + (splits + 1) * 4e-6f * M * N * (dual ? 2 : 1) / 4.5f;
+  if (splits > 1) us += 5.0f + (splits + 1) * 4e-6f * M * N * (dual ? 2 : 1) / 4.1f;
   return us;
 }
 
@@ -576,14 +684,14 @@ hipError_t run(const DenseGemm& g, hipStream_t s) {
   const Plan p = plan_for(EPI, g.M, g.N, g.K);
   switch (p.tile) {
     case k64:
-      return run_tile<E, 64, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
-                                       dense_gemm_kernel<E, 64, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
+      return run_tile<E, 64, 128, EPI>(g, p.splits, dense_gemm_64_kernel<E, ACOL, BCOL, EPI, false>,
+                                       dense_gemm_64_kernel<E, ACOL, BCOL, EPI, true>, s);
     case k128:
-      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, false>,
-                                        dense_gemm_kernel<E, 128, 128, 2, 2, 2, ACOL, BCOL, EPI, true>, s);
+      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_128_kernel<E, 2, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_128_kernel<E, 2, ACOL, BCOL, EPI, true>, s);
     case k128Deep:
-      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_kernel<E, 128, 128, 2, 2, 3, ACOL, BCOL, EPI, false>,
-                                        dense_gemm_kernel<E, 128, 128, 2, 2, 3, ACOL, BCOL, EPI, true>, s);
+      return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_128_kernel<E, 3, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_128_kernel<E, 3, ACOL, BCOL, EPI, true>, s);
     default:
       return run_tile<E, 256, 256, EPI>(g, p.splits, dense_gemm_256_kernel<E, ACOL, BCOL, EPI, false>,
                                         dense_gemm_256_kernel<E, ACOL, BCOL, EPI, true>, s);
