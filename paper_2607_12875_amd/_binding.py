@@ -7,6 +7,7 @@ fallback of any kind: a missing library or a non-OK status raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -338,9 +339,21 @@ def _at(t, name, shape, dtype, index):
     return t.data_ptr()
 
 
-def _call(f, where, index, stream, *args):
-    """f(*args, stream) on device `index`, on its current stream if none is given."""
-    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+def _on_stream(f):
+    """With stream=, the whole call runs with that as the current stream, so that
+    what it allocates belongs to it too."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return call
+
+
+def _call(f, where, index, *args):
+    """f(*args, stream) on device `index` and its current stream."""
+    s = torch._C._cuda_getCurrentRawStream(index)
     if index == torch._C._cuda_getDevice():
         status = f(*args, s)
     else:
@@ -350,8 +363,9 @@ def _call(f, where, index, stream, *args):
         raise MoeError(status, where)
 
 
+@_on_stream
 def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1e-5, y=None, sum_out=None,
-                     stats=True, stream=None):
+                     stats=True):
     """Layer or rms norm of the rows of x [T,H] (fp32, bf16, fp16), or of x +
     residual: returns (y, s, mean, rstd).
 
@@ -375,13 +389,14 @@ def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1
         rstd = torch.empty(T, dtype=torch.float32, device=x.device)
         if kind != "rms":
             mean = torch.empty_like(rstd)
-    _call(lib().moe_norm_forward, "moe_norm_forward", i, stream, x.data_ptr(), pr, pw, pb, T, H, NORM[kind], dtype,
+    _call(lib().moe_norm_forward, "moe_norm_forward", i, x.data_ptr(), pr, pw, pb, T, H, NORM[kind], dtype,
           eps, py, ps, _ptr(mean), _ptr(rstd))
     return y, x if residual is None else sum_out, mean, rstd
 
 
+@_on_stream
 def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=None, need_dweight=True,
-                      need_dbias=False, workspace=None, stream=None):
+                      need_dbias=False, workspace=None):
     """Backward pass of moe_norm_forward: returns (dx, dweight, dbias), the last
     two fp32 [H] or None.
 
@@ -401,7 +416,7 @@ def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=
     dbias = torch.empty(H, dtype=f32, device=x.device) if need_dbias else None
     nws = lib().moe_norm_backward_workspace_bytes(T, H) if need_dweight or need_dbias else 0
     workspace = _workspace(workspace, nws, x) if nws else None
-    _call(lib().moe_norm_backward, "moe_norm_backward", i, stream, pdy, x.data_ptr(), pw, pm, prs, pds, T, H,
+    _call(lib().moe_norm_backward, "moe_norm_backward", i, pdy, x.data_ptr(), pw, pm, prs, pds, T, H,
           NORM[kind], dtype, pdx, _ptr(dweight), _ptr(dbias), _ptr(workspace), nws)
     return dx, dweight, dbias
 
@@ -433,7 +448,8 @@ def moe_ffn_backward_workspace_bytes(args: MoeFfnArgs) -> int:
     return lib().moe_ffn_backward_workspace_bytes(ctypes.byref(args))
 
 
-def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=None, workspace=None, stream=None):
+@_on_stream
+def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=None, workspace=None):
     """Gated feed-forward block y = (act(x w1[:I]^T) * (x w1[I:]^T)) w2^T + add on
     bf16 or fp16 x [T,H], w1 [2I,H], w2 [H,I] (H and I multiples of 8): returns
     (y, pre, workspace).
@@ -452,13 +468,14 @@ def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=
                       _at(pre, "pre", (T, 2 * I), torch.float32, i))
     at = ctypes.byref(args)
     workspace = _workspace(workspace, lib().moe_ffn_workspace_bytes(at), x)
-    _call(lib().moe_ffn_forward, "moe_ffn_forward", i, stream, at, workspace.data_ptr(),
+    _call(lib().moe_ffn_forward, "moe_ffn_forward", i, at, workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return y, pre, workspace
 
 
+@_on_stream
 def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=None, need=(True, True, True),
-                     workspace=None, stream=None):
+                     workspace=None):
     """Backward pass of moe_ffn_forward from its pre: returns (dx, dw1, dw2,
     workspace), the gradients in x's type.  need says which of them are
     computed; the others are None."""
@@ -474,7 +491,7 @@ def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=N
                       _at(dw2, "dw2", (H, I), dt, i))
     at = ctypes.byref(args)
     workspace = _workspace(workspace, lib().moe_ffn_backward_workspace_bytes(at), x)
-    _call(lib().moe_ffn_backward, "moe_ffn_backward", i, stream, at, workspace.data_ptr(),
+    _call(lib().moe_ffn_backward, "moe_ffn_backward", i, at, workspace.data_ptr(),
           workspace.numel() * workspace.element_size())
     return dx, dw1, dw2, workspace
 

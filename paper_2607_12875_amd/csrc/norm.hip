@@ -19,6 +19,7 @@ namespace moe {
 
 namespace {
 
+constexpr int kLaunchRows = 1 << 21;  // of the forward pass
 constexpr int kMostLds = 158 * 1024;  // column sums in LDS, beside 256 bytes of its own
 constexpr int kNormBlocks = 256;  // workgroups of the backward pass at most: one per CU
 
@@ -399,15 +400,30 @@ template <class F> hipError_t with_nv(int nv, F f) {
 }
 
 template <class E, int KIND>
-hipError_t forward(const NormForward& a, hipStream_t s) {
+hipError_t forward(NormForward a, hipStream_t s) {
   // few rows: as many threads as a row can use; many: two chunks each (8192 x 7168
   // bf16 with residual 86 us, with four 92, 777 x 5120 7.2, with one 9.0)
   const Shape p = shape_of(a.H, Chunk<E>::W, a.T >= 512 ? 2 : 1);
   const int rows = std::max(1, 256 / p.G), threads = rows * p.G;
-  return with_nv(p.NV, [&](auto nv) {
-    norm_forward_kernel<E, decltype(nv)::value, KIND><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a, p.G);
-    return hipGetLastError();
-  });
+  // a launch has fewer than 2^32 threads
+  for (int left = a.T; left > 0; left -= kLaunchRows) {
+    a.T = std::min(left, kLaunchRows);
+    const hipError_t e = with_nv(p.NV, [&](auto nv) {
+      norm_forward_kernel<E, decltype(nv)::value, KIND><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a, p.G);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    const size_t n = static_cast<size_t>(a.T) * a.H;
+    a.x = static_cast<const E*>(a.x) + n;
+    a.y = static_cast<E*>(a.y) + n;
+    if (a.residual) {
+      a.residual = static_cast<const E*>(a.residual) + n;
+      a.sum = static_cast<E*>(a.sum) + n;
+    }
+    if (a.mean) a.mean += a.T;
+    if (a.rstd) a.rstd += a.T;
+  }
+  return hipSuccess;
 }
 
 template <class E, int KIND>

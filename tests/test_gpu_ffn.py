@@ -268,3 +268,47 @@ def test_pre_norm_block(T, H, I):
     shared, _, _ = moe.moe_ffn_forward(n, d["w1"], d["w2"], add=routed, y=routed, workspace=ws)
     assert shared is routed
     check("shared", shared, want["y"], rounded(want["y"], want["e_y"], BF16))
+
+
+def test_ffn_stream_argument():
+    """stream= runs the whole call there, its allocations too, behind that stream's own work."""
+    require_gpu()
+    d = _inputs(300, 520, 264, BF16)
+    y, pre, _ = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True)
+    ref = (y, pre) + moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre)[:3]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        y, pre, _ = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True, stream=side)
+        out = (y, pre) + moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, stream=side)[:3]
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(out, ref))
+
+
+def test_ffn_offsets_past_32_bits():
+    """pre and dpre of 2.3e9 elements: the last rows against the reference of those rows."""
+    require_gpu()
+    T, H, I, n = 140001, 64, 8200, 300
+    d = _inputs(T, H, I, BF16)
+    y, pre, ws = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True)
+    dx, dw1, dw2, _ = moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, workspace=ws)
+    x, dy = d["x"][-n:], d["dy"][-n:]
+    f = ffn_reference(x, d["w1"], d["w2"], None, "silu")
+    check("pre", pre[-n:], f["pre"], f["e_pre"])
+    check("y", y[-n:], f["y"], rounded(f["y"], f["e_y"], BF16))
+    b = ffn_backward_reference(dy, x, d["w1"], d["w2"], "silu")
+    check("dx", dx[-n:], b["dx"], rounded(b["dx"], b["e_dx"], BF16))
+    # a few columns of the weights' gradients, over all rows
+    c = torch.tensor([0, 17, I - 1], device="cuda")
+    w1 = torch.cat([d["w1"][c], d["w1"][I + c]])
+    part = ffn_backward_reference(d["dy"], d["x"], w1, d["w2"][:, c], "silu")
+    check("dw2", dw2[:, c], part["dw2"], rounded(part["dw2"], part["e_dw2"], BF16))
+    check("dw1", dw1[torch.cat([c, I + c])], part["dw1"], rounded(part["dw1"], part["e_dw1"], BF16))
+
+
+@pytest.mark.parametrize("T", [12, 28, 48, 200])
+def test_ffn_widest(T):
+    """H and I where the offsets of a tile's rows are largest."""
+    require_gpu()
+    _check_both(T, 65536, 64, BF16, "silu", add=True)
+    _check_both(T, 64, 65536, F16, "gelu", add=False)

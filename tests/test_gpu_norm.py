@@ -210,3 +210,62 @@ def test_norm_captured():
         got = [t.clone() for t in out]
         assert all(torch.equal(p, q) for p, q in zip(got, both()))
         torch.cuda.synchronize()
+
+
+def test_norm_stream_argument():
+    """stream= runs the whole call there, its allocations too, behind that stream's own work."""
+    require_gpu()
+    d = _inputs(700, 3000, BF16)
+    ref = moe.moe_norm_forward(d["x"], d["weight"], bias=d["bias"])
+    rb = moe.moe_norm_backward(d["dy"], d["x"], d["weight"], ref[2], ref[3], need_dbias=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        y, s, mean, rstd = moe.moe_norm_forward(d["x"], d["weight"], bias=d["bias"], stream=side)
+        b = moe.moe_norm_backward(d["dy"], s, d["weight"], mean, rstd, need_dbias=True, stream=side)
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip((y, mean, rstd) + b, (ref[0], ref[2], ref[3]) + rb))
+
+
+@pytest.mark.parametrize("H,dt", [(16384, BF16), (12000, F32), (40008, F16)])
+def test_norm_wide_captured(H, dt):
+    """The forms that keep column sums in LDS and in spilled registers, replayed."""
+    require_gpu()
+    d = _inputs(600, H, dt)
+
+    def both():
+        y, s, mean, rstd = moe.moe_norm_forward(d["x"], d["weight"], kind="rms")
+        return (y,) + moe.moe_norm_backward(d["dy"], s, d["weight"], None, rstd, kind="rms")[:2]
+
+    graph = torch.cuda.CUDAGraph()
+    both()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = both()
+    for seed in (5, 6):
+        for k, v in _inputs(600, H, dt, seed).items():
+            d[k].copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        assert all(torch.equal(p, q) for p, q in zip(got, both()))
+
+
+def test_norm_offsets_past_32_bits():
+    """2.3e9 elements: the last rows, whose offsets pass 2^31 elements, as they come alone."""
+    require_gpu()
+    T, H = 70001, 32776
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(T, H, generator=g, device="cuda", dtype=BF16)
+    w = torch.randn(H, generator=g, device="cuda").to(BF16)
+    y, _, _, rstd = moe.moe_norm_forward(x, w, kind="rms")
+    last = x[-600:].clone()
+    y2, _, _, rstd2 = moe.moe_norm_forward(last, w, kind="rms")
+    assert torch.equal(y[-600:], y2) and torch.equal(rstd[-600:], rstd2)
+    dx, dw, _ = moe.moe_norm_backward(y, x, w, None, rstd, kind="rms")
+    dx2, _, _ = moe.moe_norm_backward(y2, last, w, None, rstd2, kind="rms")
+    assert torch.equal(dx[-600:], dx2)
+    xhat = x[:, 7].double() * rstd.double()
+    want, scale = (y[:, 7].double() * xhat).sum(), (y[:, 7].double() * xhat).abs().sum()
+    # a term: three roundings of xhat and rstd's own (bounded in test_norm_wide), then T / 256 + 64 additions
+    assert abs(float(dw[7]) - float(want)) <= (T / 256 + 64 + 8) * 2.0 ** -24 * float(scale)
