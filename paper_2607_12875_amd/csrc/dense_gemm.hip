@@ -380,14 +380,15 @@ __global__ __launch_bounds__(256, 2) void dense_gemm_128_kernel(DenseGemm g, int
   epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
 }
 
-// 64 x 128 tile, four waves of 32 x 64, three buffers of kBK.  A wave's substep has
-// two products, 64 cycles, fewer than an LDS read takes, so the fragments of a whole
+// 64 x 128 or 64 x 64 tile (the small one where there are few), four waves of 32 x 64
+// or 32 x 32, three buffers of kBK.  A wave's substep has one or two products, 32 or 64
+// cycles, fewer than an LDS read takes, so the fragments of a whole
 // step are read during the step before (512 x 2048 x 1408: 8.8 us, one substep ahead
 // 10.8; 128 x 7168 x 2048 11.2 and 14.0).  A stage's buffer is free once every wave
 // has its fragments, at the barrier that opens its step, and stage kt + 3 goes there.
-template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+template <class E, int BN, bool ACOL, bool BCOL, int EPI, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void dense_gemm_64_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
-  constexpr int BM = 64, BN = 128, WM = 2, WN = 2, STAGES = 3;
+  constexpr int BM = 64, WM = 2, WN = 2, STAGES = 3;
   using W = Waves<BM, BN, WM, WN, EPI>;
   using A = Operand<BM, ACOL, W::NW, 1>;
   using B = Operand<BN, BCOL, W::NW, W::DUAL ? 2 : 1>;
@@ -609,39 +610,41 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseGemm g, int splits)
 namespace {
 
 // Which tile, and in how many parts of K.
-enum Tile { k64, k128, k128Deep, k256 };
+enum Tile { kSmall, k64, k128, k128Deep, k256 };
 struct Plan {
   Tile tile;
   int splits;
 };
 struct TileCost {
   int rows, cols, slots;  // tile, and how many run at once on the chip (256 CUs)
-  float start, alone, full;  // us: launch, first loads and epilogue; a step with one per CU, and with every slot taken
+  // us: launch, first loads and epilogue; a step with one, two and more per CU
+  float start, one, two, more;
 };
-// 64 x 128 (three buffers) and 128 x 128 (two) run two to a CU, 128 x 128 with
-// three buffers and 256 x 256 one.  Fitted to 400 timings of products of 40 to 2048
-// rows; what the figures choose takes 2 % more than the quickest on average, 15 % at
-// worst.  Among them, us, on 64-, 128-, 128- (three buffers) and 256-row tiles: 128 x
-// 7168 x 2048 11.4, 18.4, 15.3, -; 777 x 4096 x 2816 29.1, 31.3, 24.5, 54; 2048 x 4096
-// x 2816 60, 48, 54, 63; 2816 x 4096 x 2048 63, 57, 57, 52.
+// 64 x 64 and 64 x 128 (three buffers) and 128 x 128 (two) run three, two and two to a
+// CU, 128 x 128 with three buffers and 256 x 256 one.  Fitted to 1900 timings of 104
+// products, of 20 to 8000 rows: what the figures choose takes 1 % more than the
+// quickest on average.  Among them, us, on the five in this order: 512 x 2048 x 1408 7.3,
+// 8.8, 11.8, 11.8, 29.9; 777 x 4096 x 2816 36, 30, 32, 25, 55; 2048 x 4096 x 2816 77, 64,
+// 51, 54, 62; 2816 x 4096 x 2048 76, 67, 58, 59, 52.
 constexpr TileCost kTiles[] = {
-    {64, 128, 512, 4.0f, 0.26f, 0.56f},
-    {128, 128, 512, 4.7f, 0.49f, 0.86f},
-    {128, 128, 256, 4.5f, 0.43f, 0.43f},
-    {256, 256, 256, 10.4f, 1.14f, 1.14f},
+    {64, 64, 768, 3.5f, 0.20f, 0.44f, 0.63f},
+    {64, 128, 512, 3.5f, 0.29f, 0.76f, 0.76f},
+    {128, 128, 512, 4.8f, 0.48f, 0.87f, 0.87f},
+    {128, 128, 256, 4.1f, 0.44f, 0.44f, 0.44f},
+    {256, 256, 256, 11.9f, 1.08f, 1.08f, 1.08f},
 };
 // The time that a product takes by those figures: rounds of tiles, and where K is
 // split the launch that joins the parts and their traffic.  128 x 2048 (gate and up)
-// x 7168: 33 us whole and 19.6 in three parts; 512 x 2048 x 1408: 8.9 whole, 12.4 in
-// two.
+// x 7168: 33 us whole and 19.6 in three parts; 512 x 2048 x 1408 (64 x 128
+// tiles): 8.9 whole, 12.4 in two.
 float cost_of(const TileCost& t, bool dual, int M, int N, int K, int splits) {
   const int cols = dual ? t.cols / 2 : t.cols;
   const long tiles = static_cast<long>((M + t.rows - 1) / t.rows) * ((N + cols - 1) / cols) * splits;
   const int steps = ((K + kBK - 1) / kBK + splits - 1) / splits;
   const long rest = tiles % t.slots;
-  float us = static_cast<float>(tiles / t.slots) * (t.start + t.full * steps);
-  if (rest) us += t.start + (rest <= 256 ? t.alone : t.full) * steps;
-  if (splits > 1) us += 5.0f + (splits + 1) * 4e-6f * M * N * (dual ? 2 : 1) / 4.1f;
+  float us = static_cast<float>(tiles / t.slots) * (t.start + t.more * steps);
+  if (rest) us += t.start + (rest <= 256 ? t.one : rest <= 512 ? t.two : t.more) * steps;
+  if (splits > 1) us += 1.2f + 0.22f * splits + (splits + 1) * 4e-6f * M * N * (dual ? 2 : 1) / 3.2f;
   return us;
 }
 
@@ -650,7 +653,7 @@ Plan plan_for(int epi, int M, int N, int K) {
   const int nk = (K + kBK - 1) / kBK;
   Plan best{k64, 1};
   float least = 0.f;
-  for (int t = k64; t <= k256; ++t)
+  for (int t = dual ? k64 : kSmall; t <= k256; ++t)  // the smallest has no gate and up pairs
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (splits > 1 && (nk < 2 * splits || splits * static_cast<long>(M) * N * (dual ? 2 : 1) > 1L << 25)) break;
       const float us = cost_of(kTiles[t], dual, M, N, K, splits);
@@ -682,10 +685,15 @@ hipError_t run_tile(const DenseGemm& g, int splits, K whole, K part, hipStream_t
 template <class E, bool ACOL, bool BCOL, int EPI>
 hipError_t run(const DenseGemm& g, hipStream_t s) {
   const Plan p = plan_for(EPI, g.M, g.N, g.K);
+  if constexpr (EPI != kGlu) {
+    if (p.tile == kSmall)
+      return run_tile<E, 64, 64, EPI>(g, p.splits, dense_gemm_64_kernel<E, 64, ACOL, BCOL, EPI, false>,
+                                      dense_gemm_64_kernel<E, 64, ACOL, BCOL, EPI, true>, s);
+  }
   switch (p.tile) {
     case k64:
-      return run_tile<E, 64, 128, EPI>(g, p.splits, dense_gemm_64_kernel<E, ACOL, BCOL, EPI, false>,
-                                       dense_gemm_64_kernel<E, ACOL, BCOL, EPI, true>, s);
+      return run_tile<E, 64, 128, EPI>(g, p.splits, dense_gemm_64_kernel<E, 128, ACOL, BCOL, EPI, false>,
+                                       dense_gemm_64_kernel<E, 128, ACOL, BCOL, EPI, true>, s);
     case k128:
       return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_128_kernel<E, 2, ACOL, BCOL, EPI, false>,
                                         dense_gemm_128_kernel<E, 2, ACOL, BCOL, EPI, true>, s);

@@ -154,11 +154,12 @@ hipError_t rows(const DenseGemm& g, hipStream_t s) {
 
 // Up to 16 rows always.  A second fragment of rows takes the registers that keep
 // the weights coming, which costs large weights more than the tile kernels' split of
-// K and their joining launch: 17 rows, 4096 x 1408, 14.4 us here and 21.5 there, 32
-// rows, 7168 x 2048, 30.5 and 30.5, 32 rows, 4096 x 11264, 91 and 66.
+// K and their joining launch: 17 rows, 4096 x 1408, 14.4 us here and 17.7 there, 24
+// rows, 2048 x 1408, 11.7 and 15.7, 32 rows, 5120 x 1536, 22.4 and 20.4, 7168 x 2048,
+// 30.2 and 25.5.
 bool dense_rows_fits(int layout, int epi, int M, int N, int K) {
   if (layout != kRowRow || epi == kDglu || M > 32) return false;
-  return M <= 16 || static_cast<long>(N) * K * (epi == kGlu ? 2 : 1) <= 1L << 25;
+  return M <= 16 || static_cast<long>(N) * K * (epi == kGlu ? 2 : 1) <= 3L << 22;
 }
 
 hipError_t launch_dense_rows(int dtype, int epi, const DenseGemm& g, hipStream_t s) {
