@@ -4,9 +4,9 @@
 //   forward   pre = x W1^T -> h = act(gate) * up in the epilogue;  y = h W2^T (+ add)
 //   backward  dh = dy W2 -> dpre = [dh u act'(g), dh act(g)] and h in the epilogue;
 //             dx = dpre W1;  dW1 = dpre^T x;  dW2 = dy^T h
-// One tile kernel serves the six: an operand lies in memory with its reduction
-// index innermost (a row operand) or outermost (a column operand), and goes to
-// LDS as it lies.  A fragment of a row operand is one ds_read_b128; of a column
+// Three tile kernels (64, 128 and 256 rows) take each of the six: an operand lies in
+// memory with its reduction index innermost (a row operand) or outermost (a column
+// operand), and goes to LDS as it lies.  A fragment of a row operand is one ds_read_b128; of a column
 // operand two ds_read_b64_tr_b16, which transpose 4 x 16 blocks on the way.
 #include <algorithm>
 #include <utility>
@@ -98,7 +98,9 @@ struct Operand {
       desc[0] = buffer_of(base, k + kBK <= K ? whole : k < K ? tail : 0u);
       base += static_cast<uint64_t>(ld) * kBK * 2;
     } else {
-      soff = k * 2u;
+      // past the end the offset stays zero: the bounds check takes it off the
+      // buffer's length, which one row's buffer would not have left
+      soff = k < K ? k * 2u : 0u;
       if (k + kBK > K) {  // uniform
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) voff[i] = k + chunk * 8 >= K ? 0x80000000u : voff[i];
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(256, 2) void dense_gemm_64_kernel(DenseGemm g, int 
 // buffers, B three, all of the 160 KB: A's copies follow the barrier that frees
 // their buffer, B's, for a stage further on, come in the half step after, so that
 // no copy has less than three quarters of a step to land.  8192 tokens, 4096 x
-// 11264: y = h W2^T runs the matrix pipe 75 % of the cycles (67 with eight waves of
+// 11264: y = h W2^T runs the matrix pipe 78 % of the cycles (67 with eight waves of
 // 128 x 64 in two groups half a step apart, 61 with eight in step), dx 79 %.
 template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
