@@ -56,14 +56,14 @@ __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcp
 // GELU (tanh form): 0.5 (1 + tanh z) = logistic(2 z), z = c (g + 0.044715 g^3),
 // c = sqrt(2 / pi): a = g s, slope s + g s (1 - s) 2 c (1 + 3 * 0.044715 g^2).
 // Past |g| = 16 that logistic is 0 or 1 in fp32, so its argument and g times the
-// argument's slope (gdz) are taken there.
+// argument's slope (gdz) are taken there.  A NaN stays one, in the slope too.
 constexpr float kGelu2C = 1.5957691216057308f, kGeluA = 0.044715f;
 __device__ __forceinline__ float act_arg(int act, float g, float& gdz) {
   if (act == kSilu) {
     gdz = g;
     return g;
   }
-  const float c = fminf(fmaxf(g, -16.0f), 16.0f), q = kGeluA * c * c, k = kGelu2C * c;
+  const float c = g > 16.0f ? 16.0f : g < -16.0f ? -16.0f : g, q = kGeluA * c * c, k = kGelu2C * c;
   gdz = k * fmaf(3.0f, q, 1.0f);
   return k * (q + 1.0f);
 }

@@ -312,3 +312,18 @@ def test_ffn_widest(T):
     require_gpu()
     _check_both(T, 65536, 64, BF16, "silu", add=True)
     _check_both(T, 64, 65536, F16, "gelu", add=False)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T", [5, 300])
+def test_ffn_nan_gates_show(T, act):
+    """A NaN gate is seen in every gradient that it feeds, the gate's own among them, and in no other row."""
+    require_gpu()
+    d = _inputs(T, 72, 40, BF16)
+    _, pre, _ = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], act=act, save=True)
+    dx0, dw10, _, _ = moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, act=act)
+    pre[2, 7] = float("nan")
+    dx, dw1, dw2, _ = moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, act=act)
+    assert dx[2].isnan().all() and dw1[7].isnan().all() and dw1[47].isnan().all() and dw2[:, 7].isnan().all()
+    rows, cols = [i for i in range(T) if i != 2], [i for i in range(80) if i not in (7, 47)]
+    assert torch.equal(dx[rows], dx0[rows]) and torch.equal(dw1[cols], dw10[cols])
