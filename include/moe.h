@@ -334,7 +334,9 @@ moe_status moe_forward_static_ws(const moe_args* a, hipStream_t stream);
  * router or of a feed-forward block, and the gated feed-forward block (a shared
  * expert beside the routed ones, or the dense layers of a model).  As for every
  * entry point, arrays are dense and row-major, device pointers 16-byte aligned,
- * and nothing is allocated, synchronised or copied to the host.  Every sum and
+ * and nothing is allocated, synchronised or copied to the host.  No output and no
+ * workspace overlaps another array of its call but where that is said
+ * (MOE_ERR_UNSUPPORTED).  Every sum and
  * statistic is held in fp32, in a fixed order: results are the same on every
  * run.  Infinities and NaN of a row stay in what that row feeds: its own outputs
  * and the weights' gradients.
@@ -359,11 +361,13 @@ typedef enum {
  *           not written and may be NULL)
  *   weight, bias         device, dtype [H]; bias NULL for none (rms: must be)
  *   mean, rstd           device, fp32 [T], for the backward pass; each may be NULL
+ *           (rms: mean is not written)
  *   0 <= T <= MOE_MAX_ROWS, 1 <= H <= MOE_MAX_WIDTH (any: rows need no alignment of
  *   their own), eps >= 0 and finite.  T == 0 is a no-op.
  * y or sum may be x or residual itself (each row is read before it is written),
- * but not both the same array; no other overlap.
- * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (kind, dtype, eps, a bias with rms),
+ * but not both the same array.
+ * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (kind, dtype, eps, a bias with rms,
+ * an overlap),
  * MOE_ERR_NULL, MOE_ERR_ALIGN, MOE_ERR_HIP.
  */
 moe_status moe_norm_forward(const void* x, const void* residual, const void* weight, const void* bias, int T, int H,
@@ -383,7 +387,7 @@ size_t moe_norm_backward_workspace_bytes(int T, int H);
  *   mean, rstd  device, fp32 [T], as the forward pass wrote them (mean may be NULL for rms)
  *   dsum        device, dtype [T,H] or NULL: the gradient that reaches sum on its
  *               other way; dx is then the gradient of x and of residual alike
- *   dx          device, dtype [T,H]; may be dy or dsum itself, no other overlap
+ *   dx          device, dtype [T,H]; may be dy or dsum itself
  *   dweight, dbias  device, fp32 [H]; each may be NULL.  T == 0 writes zeros.
  *   ws          moe_norm_backward_workspace_bytes(T, H) bytes, unused (may be NULL)
  *               without dweight and dbias
@@ -419,7 +423,7 @@ typedef struct {
   const void* w1;  /* [2I,H]                                               */
   const void* w2;  /* [H,I]                                                */
   const void* add; /* forward: [T,H] or NULL; may be y itself              */
-  void* y;         /* forward: [T,H]                                       */
+  void* y;         /* forward: [T,H]; may be x itself                      */
   float* pre;      /* fp32 [T,2I]: forward writes it (NULL: not kept), backward reads it */
   const void* dy;  /* backward: [T,H]                                      */
   void* dx;        /* backward: [T,H], [2I,H], [H,I]; each may be NULL:    */
@@ -433,7 +437,7 @@ size_t moe_ffn_workspace_bytes(const moe_ffn_args* a);
 size_t moe_ffn_backward_workspace_bytes(const moe_ffn_args* a);
 
 /*
- * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (dtype, act), MOE_ERR_NULL,
+ * Errors: MOE_ERR_SHAPE, MOE_ERR_UNSUPPORTED (dtype, act, an overlap), MOE_ERR_NULL,
  * MOE_ERR_ALIGN, MOE_ERR_WORKSPACE, MOE_ERR_HIP.  T == 0 is a no-op forward; backward
  * it writes zero weight gradients.
  */

@@ -342,10 +342,14 @@ def _at(t, name, shape, dtype, index):
 def _on_stream(f):
     """With stream=, the whole call runs with that as the current stream, so that
     what it allocates belongs to it too."""
+    first = f.__code__.co_varnames[0]
+
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
         if stream is None:
             return f(*args, **kw)
+        if (args[0] if args else kw[first]).get_device() != stream.device_index:
+            raise ValueError(f"{first}: expected a tensor on the stream's device, cuda:{stream.device_index}")
         with torch.cuda.stream(stream):
             return f(*args, **kw)
     return call

@@ -4,6 +4,7 @@
 // allocates, synchronises or keeps state.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "../../include/moe.h"
 #include "dense.hpp"
@@ -19,6 +20,22 @@ bool aligned16(const P*... p) {
   return ((reinterpret_cast<uintptr_t>(p) | ...) & 15u) == 0;
 }
 
+// An array's bytes; none of them where it is NULL or not used.
+struct Span {
+  uintptr_t p;
+  size_t n;
+  Span(const void* at, size_t bytes) : p(reinterpret_cast<uintptr_t>(at)), n(at ? bytes : 0) {}
+};
+// Whether `out` meets none of the others, but for those in `same` that start where it does.
+bool apart(Span out, std::initializer_list<Span> others, std::initializer_list<Span> same = {}) {
+  auto meet = [&](const Span& o) { return o.n && out.n && out.p < o.p + o.n && o.p < out.p + out.n; };
+  for (const Span& o : others)
+    if (meet(o)) return false;
+  for (const Span& o : same)
+    if (o.p != out.p && meet(o)) return false;
+  return true;
+}
+
 bool norm_sizes(int T, int H) { return T >= 0 && T <= MOE_MAX_ROWS && H >= 1 && H <= MOE_MAX_WIDTH; }
 
 moe_status check_norm(int T, int H, int kind, int dtype) {
@@ -27,6 +44,8 @@ moe_status check_norm(int T, int H, int kind, int dtype) {
   if (dtype != MOE_DT_F32 && dtype != MOE_DT_BF16 && dtype != MOE_DT_F16) return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
 }
+
+size_t bytes_of(int dtype) { return dtype == MOE_DT_F32 ? 4 : 2; }
 
 bool ffn_sizes(const moe_ffn_args* a) {
   return a->T >= 0 && a->T <= MOE_MAX_ROWS && a->H >= 8 && a->H <= MOE_MAX_WIDTH && a->H % 8 == 0 && a->I >= 8 &&
@@ -40,6 +59,15 @@ moe_status check_ffn(const moe_ffn_args* a) {
   if (a->act != MOE_ACT_SILU && a->act != MOE_ACT_GELU_TANH) return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
 }
+
+// The arrays of a block's call.
+struct FfnSpans {
+  Span x, w1, w2, pre, ws;
+  FfnSpans(const moe_ffn_args* a, const void* at, size_t ws_bytes)
+      : x(a->x, rows(a) * a->H * 2), w1(a->w1, size_t{4} * a->I * a->H), w2(a->w2, size_t{2} * a->I * a->H),
+        pre(a->pre, rows(a) * a->I * 8), ws(at, ws_bytes) {}
+  static size_t rows(const moe_ffn_args* a) { return static_cast<size_t>(a->T); }
+};
 
 // Workspace: forward h, then the partial products of a split K; backward dpre, h,
 // then those.  Offsets from the start.
@@ -82,6 +110,12 @@ moe_status moe_norm_forward(const void* x, const void* residual, const void* wei
   if (T == 0) return MOE_OK;
   if (!x || !weight || !y || (residual && !sum)) return MOE_ERR_NULL;
   if (!aligned16(x, residual, weight, bias, y, sum) || !aligned16(mean, rstd)) return MOE_ERR_ALIGN;
+  const size_t n = static_cast<size_t>(T) * H * bytes_of(dtype), row = H * bytes_of(dtype), stat = static_cast<size_t>(T) * 4;
+  const Span sx{x, n}, sr{residual, n}, sw{weight, row}, sb{bias, row}, sy{y, n}, ss{residual ? sum : nullptr, n},
+      sm{kind == MOE_NORM_LAYER ? mean : nullptr, stat}, srs{rstd, stat};
+  if (!apart(sy, {sw, sb, ss, sm, srs}, {sx, sr}) || !apart(ss, {sw, sb, sm, srs}, {sx, sr}) ||
+      !apart(sm, {sx, sr, sw, sb, srs}) || !apart(srs, {sx, sr, sw, sb}))
+    return MOE_ERR_UNSUPPORTED;
   const moe::NormForward a{x, residual, weight, bias, T, H, eps, y, sum, mean, rstd};
   return moe::launch_norm_forward(dtype, kind, a, stream) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -102,6 +136,13 @@ moe_status moe_norm_backward(const void* dy, const void* x, const void* weight, 
   if (T == 0 && !sums) return MOE_OK;
   const size_t need = sums ? align_up(moe::norm_backward_workspace_bytes(T, H)) : 0;
   if (need && (!ws || ws_bytes < need)) return MOE_ERR_WORKSPACE;
+  const size_t n = static_cast<size_t>(T) * H * bytes_of(dtype), row = H * bytes_of(dtype), stat = static_cast<size_t>(T) * 4,
+               column = static_cast<size_t>(H) * 4;
+  const Span sdy{dy, n}, sx{x, n}, sw{weight, row}, sm{kind == MOE_NORM_LAYER ? mean : nullptr, stat}, srs{rstd, stat},
+      sds{dsum, n}, sdw{dweight, column}, sdb{dbias, column}, sws{ws, need};
+  if (!apart({dx, n}, {sx, sw, sm, srs, sdw, sdb, sws}, {sdy, sds}) || !apart(sdw, {sdy, sx, sw, sm, srs, sds, sdb, sws}) ||
+      !apart(sdb, {sdy, sx, sw, sm, srs, sds, sws}) || !apart(sws, {sdy, sx, sw, sm, srs, sds}))
+    return MOE_ERR_UNSUPPORTED;
   const moe::NormBackward a{dy, x, weight, dsum, mean, rstd, T, H, dx, dweight, dbias, sums ? static_cast<float*>(ws) : nullptr};
   return moe::launch_norm_backward(dtype, kind, a, stream) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -121,6 +162,11 @@ moe_status moe_ffn_forward(const moe_ffn_args* a, void* ws, size_t ws_bytes, hip
   const FfnLayout L = forward_layout(a);
   if (!ws || ws_bytes < L.total) return MOE_ERR_WORKSPACE;
   if (!aligned16(ws)) return MOE_ERR_ALIGN;
+  const FfnSpans sp(a, ws, L.total);
+  const Span add{a->add, sp.x.n};
+  if (!apart({a->y, sp.x.n}, {sp.w1, sp.w2, sp.pre, sp.ws}, {sp.x, add}) || !apart(sp.pre, {sp.x, sp.w1, sp.w2, add, sp.ws}) ||
+      !apart(sp.ws, {sp.x, sp.w1, sp.w2, add}))
+    return MOE_ERR_UNSUPPORTED;
 
   moe::DenseGemm g{};
   g.act = a->act;
@@ -152,6 +198,13 @@ moe_status moe_ffn_backward(const moe_ffn_args* a, void* ws, size_t ws_bytes, hi
   const FfnLayout L = backward_layout(a);
   if (L.total && (!ws || ws_bytes < L.total)) return MOE_ERR_WORKSPACE;
   if (!aligned16(ws)) return MOE_ERR_ALIGN;
+  const FfnSpans sp(a, ws, L.total);
+  const size_t n = static_cast<size_t>(a->T) * a->H * 2;
+  const Span dy{a->dy, n}, x{a->dw1 ? a->x : nullptr, n}, w1{a->dx ? a->w1 : nullptr, sp.w1.n}, dx{a->dx, n},
+      dw1{a->dw1, sp.w1.n}, dw2{a->dw2, sp.w2.n};
+  if (!apart(dx, {dy, x, w1, sp.w2, sp.pre, dw1, dw2, sp.ws}) || !apart(dw1, {dy, x, w1, sp.w2, sp.pre, dw2, sp.ws}) ||
+      !apart(dw2, {dy, x, w1, sp.w2, sp.pre, sp.ws}) || !apart(sp.ws, {dy, x, w1, sp.w2, sp.pre}))
+    return MOE_ERR_UNSUPPORTED;
 
   moe::DenseGemm g{};
   g.act = a->act;

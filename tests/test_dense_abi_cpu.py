@@ -1,6 +1,7 @@
 """Refusals of the norm and the feed-forward block without a GPU: what the C ABI
 rejects on the host before any launch, workspace sizes, and the binding's checks."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -104,3 +105,68 @@ def test_binding_refuses_what_the_library_cannot_see():
                  lambda: moe.moe_ffn_forward(x, w1, w2), lambda: moe.moe_ffn_backward(x, x, w1, w2, None)):
         with pytest.raises(ValueError):  # host tensors
             call()
+
+
+def test_binding_refuses_a_stream_of_another_device():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    other = types.SimpleNamespace(device_index=1)
+    for call in (lambda: moe.moe_norm_forward(x, x[0], stream=other), lambda: moe.moe_ffn_forward(x=x, w1=x, w2=x, stream=other),
+                 lambda: moe.moe_norm_backward(dy=x, x=x, weight=x[0], mean=None, rstd=None, stream=other),
+                 lambda: moe.moe_ffn_backward(x, x, x, x, None, stream=other)):
+        with pytest.raises(ValueError, match="stream's device, cuda:1"):
+            call()
+
+
+# Every array in a place of its own, 4 rows of 64 (and 128) elements: arrays of two bytes an element.
+SPOT = {k: (i + 1) << 32 for i, k in enumerate(
+    ("x", "residual", "weight", "bias", "y", "sum", "mean", "rstd", "dy", "dsum", "dx", "dweight", "dbias", "ws",
+     "w1", "w2", "add", "pre", "dw1", "dw2"))}
+
+
+def _refused(call, names, out, other):
+    """Whether the call refuses `out` at `other`'s start, inside it, and across its start."""
+    return all(call(**{**names, out: SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED for d in (0, 16, -16))
+
+
+def test_norm_forward_refuses_overlaps():
+    names = {k: SPOT[k] for k in ("x", "residual", "weight", "bias", "y", "sum", "mean", "rstd")}
+    for out, others in (("y", "weight bias sum mean rstd"), ("sum", "weight bias mean rstd"),
+                        ("mean", "x residual weight bias rstd"), ("rstd", "x residual weight bias")):
+        for other in others.split():
+            size = {"mean": 16, "rstd": 16, "weight": 128, "bias": 128}
+            deltas = [d for d in (0, 16, -16) if -size.get(out, 512) < d < size.get(other, 512)]
+            for d in deltas:
+                assert _norm(**{**names, out: SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED, (out, other, d)
+    for out in ("y", "sum"):
+        for other in ("x", "residual"):  # the array itself is allowed, a part of it is not
+            for d in (16, -16):
+                assert _norm(**{**names, out: SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED, (out, other, d)
+
+
+def test_norm_backward_refuses_overlaps():
+    names = {k: SPOT[k] for k in ("dy", "x", "weight", "mean", "rstd", "dsum", "dx", "dweight", "dbias", "ws")}
+    for out, others in (("dx", "x weight mean rstd dweight dbias ws"), ("dweight", "dy x weight mean rstd dsum dbias ws"),
+                        ("dbias", "dy x weight mean rstd dsum ws"), ("ws", "dy x weight mean rstd dsum")):
+        for other in others.split():
+            for d in (0, -16):
+                assert _norm_back(**{**names, out: SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED, (out, other, d)
+    for other in ("dy", "dsum"):
+        for d in (16, -16):
+            assert _norm_back(**{**names, "dx": SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED, (other, d)
+
+
+@pytest.mark.parametrize("which,reads,outs", [
+    ("moe_ffn_forward", ("x", "w1", "w2", "add"), ("y", "pre")),
+    ("moe_ffn_backward", ("x", "w1", "w2", "dy", "pre"), ("dx", "dw1", "dw2"))])
+def test_ffn_refuses_overlaps(which, reads, outs):
+    names = {k: SPOT[k] for k in reads + outs + ("ws",)}
+    call = lambda **kw: _ffn(which, **kw)
+    for i, out in enumerate(outs):
+        for other in reads + outs[i + 1:] + ("ws",):
+            if out == "y" and other in ("x", "add"):
+                for d in (16, -16):
+                    assert call(**{**names, out: SPOT[other] + d}) == B.MOE_ERR_UNSUPPORTED, (out, other, d)
+            else:
+                assert _refused(call, names, out, other), (out, other)
+    for other in reads:
+        assert _refused(call, names, "ws", other), other

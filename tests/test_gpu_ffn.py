@@ -327,3 +327,15 @@ def test_ffn_nan_gates_show(T, act):
     assert dx[2].isnan().all() and dw1[7].isnan().all() and dw1[47].isnan().all() and dw2[:, 7].isnan().all()
     rows, cols = [i for i in range(T) if i != 2], [i for i in range(80) if i not in (7, 47)]
     assert torch.equal(dx[rows], dx0[rows]) and torch.equal(dw1[cols], dw10[cols])
+
+
+@pytest.mark.parametrize("T", [1, 20, 90, 1200])
+def test_ffn_output_in_place_of_input(T):
+    require_gpu()
+    d = _inputs(T, 264, 200, BF16)
+    y, pre, _ = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True)
+    x = d["x"].clone()
+    moe.moe_ffn_forward(x, d["w1"], d["w2"], y=x)
+    assert torch.equal(x, y)
+    with pytest.raises(moe.MoeError, match="UNSUPPORTED"):
+        moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, dx=d["dy"])
