@@ -2,7 +2,8 @@
 
 MoE Gate -> Fused MoE -> Weight Sum (the paper's MoE skeleton, Fig. 1 and
 Fig. 3) as hand-written HIP kernels behind the C ABI of include/moe.h (plus
-the achievable-peak probes of include/moe_peaks.h); this package is the thin
+the achievable-peak probes of include/moe_peaks.h), and its dense half, norms and
+the gated feed-forward block with their backward passes; this package is the thin
 Python binding over that library (``_binding``) and its build script
 (``build``).
 """
