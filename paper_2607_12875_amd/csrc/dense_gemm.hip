@@ -4,7 +4,7 @@
 //   forward   pre = x W1^T -> h = act(gate) * up in the epilogue;  y = h W2^T (+ add)
 //   backward  dh = dy W2 -> dpre = [dh u act'(g), dh act(g)] and h in the epilogue;
 //             dx = dpre W1;  dW1 = dpre^T x;  dW2 = dy^T h
-// Three tile kernels (64, 128 and 256 rows) take each of the six: an operand lies in
+// Four tile kernels, of 64 x 64 to 256 x 256, take each of the six: an operand lies in
 // memory with its reduction index innermost (a row operand) or outermost (a column
 // operand), and goes to LDS as it lies.  A fragment of a row operand is one ds_read_b128; of a column
 // operand two ds_read_b64_tr_b16, which transpose 4 x 16 blocks on the way.
@@ -576,6 +576,83 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
   epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
 }
 
+// 256 x 128 tile, four waves of 128 x 64, three buffers of kBK, one workgroup per CU:
+// a quarter less LDS traffic per product than 128 x 128, in half the pieces of 256 x
+// 256, for products whose tiles make one even round.  Work is spread as there: after
+// a substep's eight products come a fragment of the next substep and, every second
+// time in three of the four substeps, a copy of the stage that goes where stage kt
+// was (three copies in all four take as long, six in two of them 5 % longer).  1024 x
+// 7168 x 4096: 51.9 us, 128 x 128 57.8, 256 x 256 75.4; 4096 x 1408 x 4096 45.7, 48.9, 73.5.
+template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
+__global__ __launch_bounds__(256, 1) void dense_gemm_wide_kernel(DenseGemm g, int tiles_m, int tiles_n, int splits) {
+  constexpr int BM = 256, BN = 128;
+  using W = Waves<BM, BN, 2, 2, EPI>;
+  using A = Operand<BM, ACOL, 4, 1>;
+  using B = Operand<BN, BCOL, 4, W::DUAL ? 2 : 1>;
+  constexpr int STAGES = 3, STAGE = A::kBytes + B::kBytes, N_DMA = 12;
+  static_assert(A::kCopies + B::kCopies == N_DMA && W::TM * W::TN == 8 && W::kEpilogueBytes <= STAGES * STAGE, "four copies in three substeps");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[STAGES * STAGE];
+
+  Place p;
+  if (!place_of<BM, W::NC>(g, tiles_m, tiles_n, splits, p)) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / 2, wn = wave % 2;
+  A a;
+  B b;
+  a.start(g.a, p.m0, g.M, g.K, p.k_first, 0);
+  b.start(g.b, p.n0, g.N, g.K, p.k_first, g.N);
+  a.offsets(wave, lane);
+  b.offsets(wave, lane);
+  auto ready = [&](int kt) {
+    a.step(p.k_first + kt * kBK, p.k_end);
+    b.step(p.k_first + kt * kBK, p.k_end);
+  };
+  const uint32_t smem0 = lds_addr(smem), mine = wave * 1024;
+  auto copy = [&](auto i, uint32_t buf) {
+    if constexpr (i < A::kCopies) a.template copy<i>(buf + mine);
+    else b.template copy<i - A::kCopies>(buf + A::kBytes + mine);
+  };
+  uint32_t rd = smem0, wr = smem0;  // the buffers of stage kt and of the stage being copied
+  auto next = [&](uint32_t at) { return at + STAGE == smem0 + STAGES * STAGE ? smem0 : at + STAGE; };
+  Math<E, W, A, B> x;
+  x.start(wm * W::WTM, W::bfirst(wn), lane);
+  // substep kk, the next one's six fragments, and copies FROM .. FROM + 3 (none from N_DMA on)
+  auto substep = [&](int kk, auto from) {
+    x.multiply(kk, [&](auto n) {
+      if constexpr (n < x.R) x.read((kk + 1) % 4, n);
+      if constexpr (n % 2 == 1 && from < N_DMA) copy(std::integral_constant<int, from + n / 2>{}, wr);
+    });
+  };
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    ready(s);
+    each<N_DMA>([&](auto i) { copy(i, wr); });
+    wr = next(wr);
+  }
+  ready(STAGES - 1);
+  each<4>([&](auto i) { copy(i, wr); });
+  vm_wait<N_DMA + 4>();
+  bar();
+  x.from(rd, rd + A::kBytes);
+  x.read(0);
+  for (int kt = 0; kt < p.nk; ++kt) {
+    substep(0, std::integral_constant<int, 4>{});
+    substep(1, std::integral_constant<int, 8>{});
+    substep(2, std::integral_constant<int, N_DMA>{});
+    ready(kt + STAGES);
+    wr = rd;
+    rd = next(rd);
+    x.from(rd, rd + A::kBytes);
+    settle<N_DMA>();
+    bar();  // stage kt + 1 has landed, stage kt's buffer is free
+    substep(3, std::integral_constant<int, 0>{});
+  }
+  vm_wait<0>();
+  bar();  // no wave reads the stages any more, no copy is under way
+  epilogue<E, W, EPI, SPLIT>(g, p, wm, wn, lane, reinterpret_cast<float*>(smem) + wave * 32 * W::PITCH, x.acc);
+}
+
 // The partial products of a split K, added in the order of the splits, and the epilogue.
 template <class E, int EPI>
 __global__ __launch_bounds__(64) void dense_join_kernel(DenseGemm g, int splits) {
@@ -612,7 +689,7 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseGemm g, int splits)
 namespace {
 
 // Which tile, and in how many parts of K.
-enum Tile { kSmall, k64, k128, k128Deep, k256 };
+enum Tile { kSmall, k64, k128, k128Deep, k256x128, k256 };
 struct Plan {
   Tile tile;
   int splits;
@@ -623,16 +700,18 @@ struct TileCost {
   float start, one, two, more;
 };
 // 64 x 64 and 64 x 128 (three buffers) and 128 x 128 (two) run three, two and two to a
-// CU, 128 x 128 with three buffers and 256 x 256 one.  Fitted to 1900 timings of 104
-// products, of 20 to 8000 rows: what the figures choose takes 1 % more than the
-// quickest on average.  Among them, us, on the five in this order: 512 x 2048 x 1408 7.3,
-// 8.8, 11.8, 11.8, 29.9; 777 x 4096 x 2816 36, 30, 32, 25, 55; 2048 x 4096 x 2816 77, 64,
-// 51, 54, 62; 2816 x 4096 x 2048 76, 67, 58, 59, 52.
+// CU, 128 x 128 with three buffers, 256 x 128 and 256 x 256 one.  Fitted to 1900 timings
+// of 104 products, of 20 to 8000 rows, and for 256 x 128 of 57: what the figures choose
+// takes 1 % more than the quickest on average (3 % more without 256 x 128).  Among them,
+// us, on the six in this order: 512 x 2048 x 1408 7.6, 9.2, 12.2, 11.9, 17.4, 30.9; 777 x
+// 4096 x 2816 38, 29, 31, 23, 31, 53; 2048 x 4096 x 2816 74, 59, 46, 49, 42, 59; 2816 x 4096
+// x 2048 73, 62, 55, 54, 54, 48.
 constexpr TileCost kTiles[] = {
     {64, 64, 768, 3.5f, 0.20f, 0.44f, 0.63f},
     {64, 128, 512, 3.5f, 0.29f, 0.76f, 0.76f},
     {128, 128, 512, 4.8f, 0.48f, 0.87f, 0.87f},
     {128, 128, 256, 4.1f, 0.44f, 0.44f, 0.44f},
+    {256, 128, 256, 5.6f, 0.70f, 0.70f, 0.70f},
     {256, 256, 256, 11.9f, 1.08f, 1.08f, 1.08f},
 };
 // The time that a product takes by those figures: rounds of tiles, and where K is
@@ -702,6 +781,9 @@ hipError_t run(const DenseGemm& g, hipStream_t s) {
     case k128Deep:
       return run_tile<E, 128, 128, EPI>(g, p.splits, dense_gemm_128_kernel<E, 3, ACOL, BCOL, EPI, false>,
                                         dense_gemm_128_kernel<E, 3, ACOL, BCOL, EPI, true>, s);
+    case k256x128:
+      return run_tile<E, 256, 128, EPI>(g, p.splits, dense_gemm_wide_kernel<E, ACOL, BCOL, EPI, false>,
+                                        dense_gemm_wide_kernel<E, ACOL, BCOL, EPI, true>, s);
     default:
       return run_tile<E, 256, 256, EPI>(g, p.splits, dense_gemm_256_kernel<E, ACOL, BCOL, EPI, false>,
                                         dense_gemm_256_kernel<E, ACOL, BCOL, EPI, true>, s);

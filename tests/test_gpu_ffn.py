@@ -339,3 +339,19 @@ def test_ffn_output_in_place_of_input(T):
     assert torch.equal(x, y)
     with pytest.raises(moe.MoeError, match="UNSUPPORTED"):
         moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, dx=d["dy"])
+
+
+@pytest.mark.parametrize("dt,act", [(BF16, "silu"), (F16, "gelu")])
+@pytest.mark.parametrize("T,H,I", [
+    (520, 1032, 2056), (520, 2056, 2056), (1000, 520, 2056), (1000, 4104, 264), (2040, 520, 2056)])
+def test_ffn_about_one_round_of_tiles(T, H, I, dt, act):
+    """Sizes whose products fill the chip once with tiles of 256 x 128, each of the six among them."""
+    require_gpu()
+    _check_both(T, H, I, dt, act, add=T % 16 == 0)
+
+
+@pytest.mark.parametrize("T,H,I", [(1000, 6152, 1032), (1000, 6152, 2056), (1000, 2056, 8200), (5000, 1032, 2056)])
+def test_ffn_long_sums_in_parts(T, H, I):
+    """Few tiles and long sums: products whose sums are split, each of the six among them."""
+    require_gpu()
+    _check_both(T, H, I, BF16, "silu", add=True)
