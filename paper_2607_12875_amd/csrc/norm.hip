@@ -247,7 +247,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackward a, int
       float* const sw = joined + (gt + i * G) * W;
       const bool mine = (gt + i * G) * W < a.H;
 #pragma unroll
-      for (int e = 0; e < W; ++e) x[i][e] = (x[i][e] - mean) * rstd;
+      for (int e = 0; e < W; ++e)  // past the row an exact zero: -mean * rstd may be past fp32
+        x[i][e] = KIND != kLayerNorm || (gt + i * G) * W + e < a.H ? (x[i][e] - mean) * rstd : 0.f;
       if constexpr (IN_LDS) {
         if (mine) {
 #pragma unroll

@@ -269,3 +269,26 @@ def test_norm_offsets_past_32_bits():
     want, scale = (y[:, 7].double() * xhat).sum(), (y[:, 7].double() * xhat).abs().sum()
     # a term: three roundings of xhat and rstd's own (bounded in test_norm_wide), then T / 256 + 64 additions
     assert abs(float(dw[7]) - float(want)) <= (T / 256 + 64 + 8) * 2.0 ** -24 * float(scale)
+
+
+@pytest.mark.parametrize("H,dt", [(100, F32), (100, BF16), (1004, F32), (9000, F32), (20003, BF16), (40008, BF16), (30001, F32)])
+def test_norm_backward_far_mean(H, dt):
+    """A constant row whose mean times rstd is past fp32: xhat is zero, and what lies past the row counts nothing."""
+    require_gpu()
+    print(f"far mean H={H} {dt}", flush=True)
+    c, eps = 2.0 ** 110, 1e-12  # sums of up to H such values are exact in fp32; rstd is a million
+    d = _inputs(21, H, dt)
+    x = torch.full((21, H), c, dtype=dt, device="cuda")
+    y, _, mean, rstd = moe.moe_norm_forward(x, d["weight"], bias=d["bias"], eps=eps)
+    assert torch.equal(y, d["bias"].expand(21, H)) and (mean == c).all()
+    assert ((mean.double() * rstd.double()) > torch.finfo(F32).max).all()
+    dx, dw, db = moe.moe_norm_backward(d["dy"], x, d["weight"], mean, rstd, need_dbias=True)
+    g, r = d["dy"].double() * d["weight"].double(), rstd.double()[:, None]
+    s1 = g.mean(1, keepdim=True)
+    want = r * (g - s1)
+    # the product's rounding, the row sum's and the mean's, the differences', the last product's
+    err = r * 2.0 ** -24 * ((64 + 6 + 16 + 4) * g.abs().mean(1, keepdim=True) + 4 * (g.abs() + s1.abs())) + 2.0 ** -23 * want.abs()
+    check("dx", dx, want, rounded(want, err, dt))
+    assert not dw.any()
+    b, scale = d["dy"].double().sum(0), d["dy"].double().abs().sum(0)
+    check("dbias", db, b, (21 / 256 + 64 + 1) * 2.0 ** -24 * scale)
