@@ -375,7 +375,7 @@ moe_status moe_norm_forward(const void* x, const void* residual, const void* wei
                             hipStream_t stream);
 
 /* Workspace of moe_norm_backward where dweight or dbias is asked for; 0 for sizes
- * it refuses. */
+ * it refuses.  Never less for more rows. */
 size_t moe_norm_backward_workspace_bytes(int T, int H);
 
 /*
@@ -432,7 +432,8 @@ typedef struct {
 } moe_ffn_args;
 
 /* Workspace of the forward and of the backward pass, from T, H, I; 0 for sizes
- * they refuse. */
+ * they refuse.  Never less for more rows: what T rows need serves any fewer.  (Sums
+ * in parts, which mostly the smaller batches take, account for up to 128 MiB.) */
 size_t moe_ffn_workspace_bytes(const moe_ffn_args* a);
 size_t moe_ffn_backward_workspace_bytes(const moe_ffn_args* a);
 

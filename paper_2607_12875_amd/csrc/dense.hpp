@@ -52,6 +52,7 @@ struct DenseGemm {
 };
 // Operand layouts of the products that the block needs.
 enum DenseLayout { kRowRow, kRowCol, kColCol };
+// Bytes of part; never fewer for more rows of the block (M, K where both operands are columns).
 size_t dense_gemm_workspace_bytes(int layout, int epi, int M, int N, int K);
 hipError_t launch_dense_gemm(int dtype, int layout, int epi, const DenseGemm& g, hipStream_t s);
 

@@ -729,14 +729,19 @@ float cost_of(const TileCost& t, bool dual, int M, int N, int K, int splits) {
   return us;
 }
 
+// K is split into one of these numbers of parts, of two steps or more, while the
+// partial products stay below 2^25 elements.
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16};
+constexpr long kMostPart = 1L << 25;
+
 Plan plan_for(int epi, int M, int N, int K) {
   const bool dual = epi == kGlu;
   const int nk = (K + kBK - 1) / kBK;
   Plan best{k64, 1};
   float least = 0.f;
   for (int t = dual ? k64 : kSmall; t <= k256; ++t)  // the smallest has no gate and up pairs
-    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      if (splits > 1 && (nk < 2 * splits || splits * static_cast<long>(M) * N * (dual ? 2 : 1) > 1L << 25)) break;
+    for (int splits : kSplits) {
+      if (splits > 1 && (nk < 2 * splits || splits * static_cast<long>(M) * N * (dual ? 2 : 1) > kMostPart)) break;
       const float us = cost_of(kTiles[t], dual, M, N, K, splits);
       if (least == 0.f || us < least) {
         least = us;
@@ -802,10 +807,20 @@ hipError_t run_type(int layout, int epi, const DenseGemm& g, hipStream_t s) {
 
 }  // namespace
 
+// What the plan for any number of the block's rows up to these may ask for, not what
+// the plan for these does: fewer rows are often split more (256 rows of 7168 x 2048
+// take 17 MB of partial products, 512 none), and a caller sizes for its largest batch.
 size_t dense_gemm_workspace_bytes(int layout, int epi, int M, int N, int K) {
   if (dense_rows_fits(layout, epi, M, N, K)) return 0;
-  const Plan p = plan_for(epi, M, N, K);
-  return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * M * N * (epi == kGlu ? 2 : 1) * 4;
+  const int nk = (K + kBK - 1) / kBK;
+  const long whole = static_cast<long>(M) * N * (epi == kGlu ? 2 : 1);
+  long most = 0;
+  for (int splits : kSplits) {
+    if (splits == 1 || nk < 2 * splits) continue;
+    if (layout != kColCol) most = std::min(splits * whole, kMostPart);  // M of them or fewer
+    else if (splits * whole <= kMostPart) most = splits * whole;        // a sum over K of them or fewer
+  }
+  return static_cast<size_t>(most) * 4;
 }
 
 hipError_t launch_dense_gemm(int dtype, int layout, int epi, const DenseGemm& g, hipStream_t s) {

@@ -170,3 +170,14 @@ def test_ffn_refuses_overlaps(which, reads, outs):
                 assert _refused(call, names, out, other), (out, other)
     for other in reads:
         assert _refused(call, names, "ws", other), other
+
+
+@pytest.mark.parametrize("H,I", [(8, 8), (256, 128), (1024, 520), (7168, 2048), (4096, 11264), (65536, 64), (64, 65536)])
+def test_workspace_for_many_rows_serves_fewer(H, I):
+    """No number of rows needs more than a larger one does."""
+    last = (0, 0, 0)
+    for T in [*range(0, 1100), *range(1100, 70000, 61), 1 << 20, 1 << 24]:
+        a = B.make_ffn_args(T, H, I)
+        need = (moe.moe_ffn_workspace_bytes(a), moe.moe_ffn_backward_workspace_bytes(a), moe.moe_norm_backward_workspace_bytes(T, H))
+        assert all(n >= m for n, m in zip(need, last)), (T, need, last)
+        last = need

@@ -355,3 +355,22 @@ def test_ffn_long_sums_in_parts(T, H, I):
     """Few tiles and long sums: products whose sums are split, each of the six among them."""
     require_gpu()
     _check_both(T, H, I, BF16, "silu", add=True)
+
+
+def test_ffn_one_workspace_for_every_batch():
+    """The workspace of the largest batch, between guard bands, serves the smaller ones, which split their sums more."""
+    require_gpu()
+    H, I, most = 2048, 1408, 700
+    a = moe.make_ffn_args(most, H, I)
+    need = max(moe.moe_ffn_workspace_bytes(a), moe.moe_ffn_backward_workspace_bytes(a))
+    base = torch.full((need + 8192,), 7, dtype=torch.uint8, device="cuda")
+    ws = base[4096:4096 + need]
+    for T in (1, 17, 40, 192, 256, 302, 512, 700):
+        d = _inputs(T, H, I, BF16)
+        y, pre, _ = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True)
+        want = (y, pre) + moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre)[:3]
+        y, pre, same = moe.moe_ffn_forward(d["x"], d["w1"], d["w2"], save=True, workspace=ws)
+        assert same is ws
+        got = (y, pre) + moe.moe_ffn_backward(d["dy"], d["x"], d["w1"], d["w2"], pre, workspace=ws)
+        assert got[-1] is ws and all(torch.equal(p, q) for p, q in zip(got, want)), T
+    assert (base[:4096] == 7).all() and (base[4096 + need:] == 7).all()
