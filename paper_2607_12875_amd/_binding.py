@@ -315,12 +315,21 @@ def moe_forward(hidden, logits, w1, w2, top_k, *, mode="softmax", renormalize=Tr
 
 
 # ------------------------------------------------- norm, feed-forward block
+def _sizes(where, *n):
+    """Refuse a size that a C int would cut, as the library refuses one past its limits."""
+    if min(n) < -1 << 31 or max(n) >= 1 << 31:
+        raise MoeError(MOE_ERR_SHAPE, where)
+
+
 def _rows(x, name):
     """Shape and device index of a contiguous [T, width] device tensor."""
     i = x.get_device()
     if i < 0 or x.dim() != 2 or not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous two-dimensional device tensor")
-    return x.shape, i
+    shape = x.shape
+    if (shape[0] | shape[1]) >> 31:
+        _sizes(name, *shape)
+    return shape, i
 
 
 def _dtype(x, name):
@@ -426,6 +435,7 @@ def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=
 
 
 def moe_norm_backward_workspace_bytes(T: int, H: int) -> int:
+    _sizes("moe_norm_backward_workspace_bytes", T, H)
     return lib().moe_norm_backward_workspace_bytes(T, H)
 
 
@@ -440,6 +450,7 @@ def _workspace(ws, need, ref):
 
 def make_ffn_args(T, H, I, *, dtype=torch.bfloat16, act="silu", x=None, w1=None, w2=None, add=None, y=None, pre=None,
                   dy=None, dx=None, dw1=None, dw2=None) -> MoeFfnArgs:
+    _sizes("make_ffn_args", T, H, I)
     return MoeFfnArgs(T, H, I, DTYPE[dtype], ACT[act], _ptr(x), _ptr(w1), _ptr(w2), _ptr(add), _ptr(y), _ptr(pre),
                       _ptr(dy), _ptr(dx), _ptr(dw1), _ptr(dw2))
 
@@ -463,6 +474,8 @@ def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=
     shape, i = _rows(x, "x")
     T, H = shape
     I, dt = w2.shape[-1], x.dtype
+    if I >> 31:
+        _sizes("w2", I)
     if y is None:
         y = torch.empty_like(x)
     if save and pre is None:
@@ -486,6 +499,8 @@ def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=N
     shape, i = _rows(x, "x")
     T, H = shape
     I, dt = w2.shape[-1], x.dtype
+    if I >> 31:
+        _sizes("w2", I)
     dx = None if not need[0] else torch.empty_like(x) if dx is None else dx
     dw1 = None if not need[1] else torch.empty_like(w1) if dw1 is None else dw1
     dw2 = None if not need[2] else torch.empty_like(w2) if dw2 is None else dw2

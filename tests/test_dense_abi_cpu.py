@@ -181,3 +181,24 @@ def test_workspace_for_many_rows_serves_fewer(H, I):
         need = (moe.moe_ffn_workspace_bytes(a), moe.moe_ffn_backward_workspace_bytes(a), moe.moe_norm_backward_workspace_bytes(T, H))
         assert all(n >= m for n, m in zip(need, last)), (T, need, last)
         last = need
+
+
+def test_binding_refuses_sizes_past_32_bits():
+    """A C int would cut 2^32 + 8 rows or columns to 8."""
+    far = (1 << 32) + 8
+
+    def tensor(*shape):
+        return types.SimpleNamespace(get_device=lambda: 0, dim=lambda: len(shape), is_contiguous=lambda: True,
+                                     shape=torch.Size(shape), dtype=torch.bfloat16)
+
+    calls = [lambda: moe.make_ffn_args(far, 64, 128), lambda: moe.make_ffn_args(4, 64, far),
+             lambda: moe.moe_norm_backward_workspace_bytes(far, 64),
+             lambda: moe.moe_ffn_forward(tensor(4, 64), None, tensor(64, far)),
+             lambda: moe.moe_ffn_backward(None, tensor(4, 64), None, tensor(64, far), None)]
+    for x in (tensor(far, 64), tensor(4, far)):
+        calls += [lambda x=x: moe.moe_norm_forward(x, None), lambda x=x: moe.moe_norm_backward(None, x, None, None, None),
+                  lambda x=x: moe.moe_ffn_forward(x, None, tensor(64, 128)),
+                  lambda x=x: moe.moe_ffn_backward(None, x, None, tensor(64, 128), None)]
+    for call in calls:
+        with pytest.raises(moe.MoeError, match="SHAPE"):
+            call()

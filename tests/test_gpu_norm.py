@@ -292,3 +292,11 @@ def test_norm_backward_far_mean(H, dt):
     assert not dw.any()
     b, scale = d["dy"].double().sum(0), d["dy"].double().abs().sum(0)
     check("dbias", db, b, (21 / 256 + 64 + 1) * 2.0 ** -24 * scale)
+
+
+def test_norm_refuses_rows_past_32_bits():
+    """2^32 + 5 rows are not taken for five."""
+    require_gpu()
+    x = torch.empty((1 << 32) + 5, 1, dtype=BF16, device="cuda")
+    with pytest.raises(moe.MoeError, match="SHAPE"):
+        moe.moe_norm_forward(x, torch.ones(1, dtype=BF16, device="cuda"))
