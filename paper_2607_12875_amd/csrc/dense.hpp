@@ -12,6 +12,7 @@ namespace moe {
 constexpr int kF32 = 0, kBf16 = 1, kF16 = 2;
 constexpr int kLayerNorm = 0, kRmsNorm = 1;
 constexpr int kSilu = 0, kGeluTanh = 1;
+constexpr int kMostWidth = 65536;  // MOE_MAX_WIDTH
 
 struct NormForward {
   const void *x, *residual, *weight, *bias;  // residual, bias: or null

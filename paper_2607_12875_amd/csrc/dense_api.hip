@@ -12,6 +12,7 @@
 namespace {
 
 constexpr size_t kAlign = 256;
+static_assert(MOE_MAX_WIDTH == moe::kMostWidth, "the widths that kernels are made for");
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 

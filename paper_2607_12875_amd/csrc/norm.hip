@@ -10,6 +10,7 @@
 // divides leaves rows off their 16-byte alignment, which the memory takes, and a
 // last chunk that is read element by element.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "dense.hpp"
@@ -390,15 +391,17 @@ int backward_blocks(int T, int groups) {
   return (sets + each - 1) / each;
 }
 
-template <class F> hipError_t with_nv(int nv, F f) {
-  switch (nv) {
-    case 1: return f(std::integral_constant<int, 1>{});
-    case 2: return f(std::integral_constant<int, 2>{});
-    case 4: return f(std::integral_constant<int, 4>{});
-    case 8: return f(std::integral_constant<int, 8>{});
-    default: return f(std::integral_constant<int, 16>{});
+// f with a thread's chunks as a constant; rows of more than 1024 W elements have
+// several, up to kMostWidth.
+template <class E, int NV = 1, class F> hipError_t with_nv(int nv, F f) {
+  if constexpr (1024 * Chunk<E>::W * NV < kMostWidth) {
+    if (nv > NV) return with_nv<E, 2 * NV>(nv, f);
   }
+  return f(std::integral_constant<int, NV>{});
 }
+
+// Bytes of both column sums of a row.
+constexpr int sums_bytes(int H) { return 2 * ((H + 7) / 8 * 8) * 4; }
 
 template <class E, int KIND>
 hipError_t forward(NormForward a, hipStream_t s) {
@@ -409,7 +412,7 @@ hipError_t forward(NormForward a, hipStream_t s) {
   // a launch has fewer than 2^32 threads
   for (int left = a.T; left > 0; left -= kLaunchRows) {
     a.T = std::min(left, kLaunchRows);
-    const hipError_t e = with_nv(p.NV, [&](auto nv) {
+    const hipError_t e = with_nv<E>(p.NV, [&](auto nv) {
       norm_forward_kernel<E, decltype(nv)::value, KIND><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a, p.G);
       return hipGetLastError();
     });
@@ -431,23 +434,27 @@ template <class E, int KIND>
 hipError_t backward(const NormBackward& a, hipStream_t s) {
   const Shape p = shape_of(a.H, Chunk<E>::W, 1);
   const int groups = p.NV > 1 ? 1 : 1024 / p.G, threads = groups * p.G, blocks = backward_blocks(a.T, groups);
-  const int sums = 2 * ((a.H + 7) / 8 * 8) * 4;
-  const bool in_lds = p.NV > 1 && sums <= kMostLds;
+  const int sums = sums_bytes(a.H);
   if (a.T > 0) {
-    const hipError_t e = with_nv(p.NV, [&](auto nv) {
-      constexpr int NV = decltype(nv)::value;
-      if constexpr (NV > 1) {
-        if (in_lds) {
+    const hipError_t e = with_nv<E>(p.NV, [&](auto nv) {
+      constexpr int NV = decltype(nv)::value, W = Chunk<E>::W;
+      // the widths that take NV chunks: does a row's pair of sums fit the LDS?
+      constexpr int least = 1024 * W * (NV / 2) + 1, most = std::min(1024 * W * NV, kMostWidth);
+      constexpr bool never = NV == 1 || sums_bytes(least) > kMostLds, always = !never && sums_bytes(most) <= kMostLds;
+      auto launch = [&](auto in_lds) {
+        constexpr bool IN_LDS = decltype(in_lds)::value;
+        if constexpr (IN_LDS) {
           const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(norm_backward_kernel<E, NV, KIND, true>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
           if (e != hipSuccess) return e;
-          norm_backward_kernel<E, NV, KIND, true><<<blocks, threads, sums, s>>>(a, p.G);
-          return hipGetLastError();
         }
-      }
-      // several row groups have one chunk per thread each
-      norm_backward_kernel<E, NV, KIND, false><<<blocks, threads, groups > 1 ? 2 * threads * Chunk<E>::W * 4 : 0, s>>>(a, p.G);
-      return hipGetLastError();
+        // several row groups have one chunk per thread each
+        const int lds = IN_LDS ? sums : groups > 1 ? 2 * threads * W * 4 : 0;
+        norm_backward_kernel<E, NV, KIND, IN_LDS><<<blocks, threads, lds, s>>>(a, p.G);
+        return hipGetLastError();
+      };
+      if constexpr (never || always) return launch(std::bool_constant<always>{});
+      else return sums <= kMostLds ? launch(std::true_type{}) : launch(std::false_type{});
     });
     if (e != hipSuccess) return e;
   }

@@ -1,6 +1,7 @@
 """Refusals of the norm and the feed-forward block without a GPU: what the C ABI
 rejects on the host before any launch, workspace sizes, and the binding's checks."""
 import ctypes
+import re
 import types
 
 import pytest
@@ -202,3 +203,23 @@ def test_binding_refuses_sizes_past_32_bits():
     for call in calls:
         with pytest.raises(moe.MoeError, match="SHAPE"):
             call()
+
+
+def test_library_holds_the_norm_forms_that_widths_choose():
+    """One kernel per form that some width takes, and no other: 1024 threads with 1, 2, 4, .. chunks of 16 bytes
+    each, and several in the backward pass with both column sums in LDS where 158 KB hold them."""
+    forward, backward = set(), set()
+    for name, w in (("f", 4), ("DF16b", 8), ("DF16_", 8)):
+        for H in range(1, 65537):
+            nv = 1
+            while 1024 * nv * w < H:
+                nv *= 2
+            forward |= {(name, nv, kind) for kind in (0, 1)}
+            backward |= {(name, nv, kind, int(nv > 1 and (H + 7) // 8 * 8 * 8 <= 158 * 1024)) for kind in (0, 1)}
+    with open(B.LIB_PATH, "rb") as f:
+        code = f.read()
+    found = {(a.decode(), int(n), int(k)) for a, n, k in re.findall(rb"norm_forward_kernelI(\w+?)Li(\d+)ELi(\d)E", code)}
+    assert found == forward
+    found = {(a.decode(), int(n), int(k), int(l))
+             for a, n, k, l in re.findall(rb"norm_backward_kernelI(\w+?)Li(\d+)ELi(\d)ELb([01])E", code)}
+    assert found == backward
