@@ -300,3 +300,35 @@ def test_norm_refuses_rows_past_32_bits():
     x = torch.empty((1 << 32) + 5, 1, dtype=BF16, device="cuda")
     with pytest.raises(moe.MoeError, match="SHAPE"):
         moe.moe_norm_forward(x, torch.ones(1, dtype=BF16, device="cuda"))
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_norm_more_rows_than_a_launch(kind):
+    """2^21 rows go with one launch of the forward pass; the next ones follow where they end."""
+    require_gpu()
+    T = (1 << 21) + 5
+    _check_both(T, 9, BF16, kind, residual=True)
+    d = _inputs(T, 9, BF16, seed=2)
+    y, s, _, rstd = moe.moe_norm_forward(d["x"], d["weight"], kind=kind)
+    last = d["x"][(1 << 21) - 8:]
+    y2, _, _, rstd2 = moe.moe_norm_forward(last, d["weight"], kind=kind)
+    assert s is d["x"] and torch.equal(y[-13:], y2) and torch.equal(rstd[-13:], rstd2)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("H", [100, 4096])
+def test_norm_zero_row_beside_others(H, kind):
+    """A row of zeros gives the bias or zero, and leaves the other rows' bits alone, forward and backward."""
+    require_gpu()
+    d = _inputs(40, H, F16)
+    bias = d["bias"] if kind == "layer" else None
+    ref = moe.moe_norm_forward(d["x"], d["weight"], bias=bias, kind=kind)
+    rb = moe.moe_norm_backward(d["dy"], d["x"], d["weight"], ref[2], ref[3], kind=kind)[0]
+    x = d["x"].clone()
+    x[7] = 0
+    y, _, mean, rstd = moe.moe_norm_forward(x, d["weight"], bias=bias, kind=kind)
+    dx = moe.moe_norm_backward(d["dy"], x, d["weight"], mean, rstd, kind=kind)[0]
+    keep = [i for i in range(40) if i != 7]
+    assert torch.equal(y[keep], ref[0][keep]) and torch.equal(dx[keep], rb[keep])
+    assert torch.equal(y[7], bias) if kind == "layer" else not y[7].any()
+    assert torch.isfinite(dx[7]).all()
