@@ -493,10 +493,11 @@ __global__ __launch_bounds__(256, 2) void dense_gemm_64_kernel(DenseGemm g, int 
 // take half of its 512 registers).  The LDS reads of the products are the fewest
 // that way, 128 KB per step; with the 64 KB that land they take most of the LDS's
 // time, so they are spread evenly: after a substep's sixteen products come, in
-// turn, a fragment of the next substep and, every fourth time, a copy.  A has two
-// buffers, B three, all of the 160 KB: A's copies follow the barrier that frees
-// their buffer, B's, for a stage further on, come in the half step after, so that
-// no copy has less than three quarters of a step to land.  8192 tokens, 4096 x
+// turn, a fragment of the next substep and, every fourth time, a copy or two.  A has
+// two buffers, B three, all of the 160 KB: A's eight copies follow the barrier that
+// frees their buffer, in the step's last quarter, B's, for a stage further on, come
+// in the half step after, none in the third quarter, so that no copy has less than
+// three quarters of a step to land.  8192 tokens, 4096 x
 // 11264: y = h W2^T runs the matrix pipe 78 % of the cycles (67 with eight waves of
 // 128 x 64 in two groups half a step apart, 61 with eight in step), dx 79 %.
 template <class E, bool ACOL, bool BCOL, int EPI, bool SPLIT>
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
   using A = Operand<256, ACOL, 4, 1>;
   using B = Operand<256, BCOL, 4, W::DUAL ? 2 : 1>;
   constexpr int NA = A::kCopies, NB = B::kCopies;
-  static_assert(NA == 8 && NB == 8 && W::kEpilogueBytes <= 2 * A::kBytes + 3 * B::kBytes, "four copies per substep");
+  static_assert(NA == 8 && NB == 8 && W::kEpilogueBytes <= 2 * A::kBytes + 3 * B::kBytes, "eight copies each");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * A::kBytes + 3 * B::kBytes];
 
   Place p;
@@ -526,15 +527,17 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
   auto ready_b = [&](int kt) { b.step(p.k_first + kt * kBK, p.k_end); };
   Math<E, W, A, B> x;
   x.start(wm * W::WTM, W::bfirst(wn), lane);
-  // substep kk, the next one's fragments, and four copies
+  // substep kk, the next one's fragments, and copy(0) .. copy(3)
   auto substep = [&](int kk, auto copy) {
     x.multiply(kk, [&](auto n) {
       if constexpr (n % 2 == 0) x.read((kk + 1) % 4, n / 2);
       else if constexpr (n % 4 == 1) copy(std::integral_constant<int, n / 4>{});
     });
   };
-  auto a_low = [&](auto c) { a.template copy<c>(wa + mine); };
-  auto a_high = [&](auto c) { a.template copy<c + 4>(wa + mine); };
+  auto a_both = [&](auto c) {
+    a.template copy<c>(wa + mine);
+    a.template copy<c + 4>(wa + mine);
+  };
   auto b_low = [&](auto c) { b.template copy<c>(wb + mine); };
   auto b_high = [&](auto c) { b.template copy<c + 4>(wb + mine); };
 
@@ -568,7 +571,7 @@ __global__ __launch_bounds__(256, 1) void dense_gemm_256_kernel(DenseGemm g, int
     x.from(ra, rb);
     settle<NB>();
     bar();  // stage kt + 1 has landed, stage kt's buffers are free
-    substep(3, [&](auto c) { a.template copy<c>(wa + mine); a.template copy<c + 4>(wa + mine); });
+    substep(3, a_both);
     ready_b(kt + 3);
   }
   vm_wait<0>();
