@@ -315,6 +315,10 @@ def moe_forward(hidden, logits, w1, w2, top_k, *, mode="softmax", renormalize=Tr
 
 
 # ------------------------------------------------- norm, feed-forward block
+# These calls and their backward passes are apart: results carry no autograd graph,
+# whether or not the inputs require gradients.  As under torch.cuda.stream, a caller
+# who frees inputs that another stream allocated before stream= has run the call
+# tells the allocator (Tensor.record_stream).
 def _sizes(where, *n):
     """Refuse a size that a C int would cut, as the library refuses one past its limits."""
     if min(n) < -1 << 31 or max(n) >= 1 << 31:
@@ -416,7 +420,8 @@ def moe_norm_backward(dy, x, weight, mean, rstd, *, kind="layer", dsum=None, dx=
     x is the s that the forward pass returned, mean and rstd its statistics
     (mean None for "rms"); dsum (or None) the gradient that reaches s on its
     other way, added to dx.  workspace: a uint8 tensor of
-    moe_norm_backward_workspace_bytes, or None to allocate one."""
+    moe_norm_backward_workspace_bytes; without, or with fewer, the call allocates
+    one for itself."""
     shape, i = _rows(x, "x")
     T, H = shape
     dt, dtype, f32 = x.dtype, _dtype(x, "x"), torch.float32
@@ -469,8 +474,10 @@ def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=
     bf16 or fp16 x [T,H], w1 [2I,H], w2 [H,I] (H and I multiples of 8): returns
     (y, pre, workspace).
 
-    With save, pre (fp32 [T,2I]) keeps both projections for moe_ffn_backward,
-    else it is None.  add [T,H] may be y itself."""
+    With save, or into a pre that is given, pre (fp32 [T,2I]) keeps both
+    projections for moe_ffn_backward, else it is None.  add [T,H] may be y itself.
+    workspace: a uint8 tensor, kept from call to call; without, or with fewer than
+    moe_ffn_workspace_bytes, a new one, which is returned."""
     shape, i = _rows(x, "x")
     T, H = shape
     I, dt = w2.shape[-1], x.dtype
@@ -495,7 +502,8 @@ def moe_ffn_backward(dy, x, w1, w2, pre, *, act="silu", dx=None, dw1=None, dw2=N
                      workspace=None):
     """Backward pass of moe_ffn_forward from its pre: returns (dx, dw1, dw2,
     workspace), the gradients in x's type.  need says which of them are
-    computed; the others are None."""
+    computed; the others are None.  workspace as for moe_ffn_forward, of
+    moe_ffn_backward_workspace_bytes."""
     shape, i = _rows(x, "x")
     T, H = shape
     I, dt = w2.shape[-1], x.dtype

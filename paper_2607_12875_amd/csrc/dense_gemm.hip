@@ -708,7 +708,9 @@ struct TileCost {
 // takes 1 % more than the quickest on average (3 % more without 256 x 128).  Among them,
 // us, on the six in this order: 512 x 2048 x 1408 7.6, 9.2, 12.2, 11.9, 17.4, 30.9; 777 x
 // 4096 x 2816 38, 29, 31, 23, 31, 53; 2048 x 4096 x 2816 74, 59, 46, 49, 42, 59; 2816 x 4096
-// x 2048 73, 62, 55, 54, 54, 48.
+// x 2048 73, 62, 55, 54, 54, 48.  They know neither the bytes of an epilogue nor that the
+// clock falls in long runs: 8192 x 4096 x 11264, 404 us by them, takes 550, and with kDglu's
+// 1.3 GB (8192 x 11264 x 4096) 840 for 486.
 constexpr TileCost kTiles[] = {
     {64, 64, 768, 3.5f, 0.20f, 0.44f, 0.63f},
     {64, 128, 512, 3.5f, 0.29f, 0.76f, 0.76f},

@@ -1,15 +1,16 @@
 // The feed-forward block's forward products for few rows (decode): C[m][n] =
 // sum_k A(m,k) B(n,k) with up to 32 rows of A.  Every weight byte is read once, and
-// that is all the time there is.  A workgroup owns sixteen rows of B (kGlu: eight
+// that is most of the time there is.  A workgroup owns sixteen rows of B (kGlu: eight
 // gate and eight up, of the same columns) and its four waves share K out in pieces
 // of 256 elements.  HBM wants long runs: a load instruction takes 512 contiguous
 // bytes of each of two rows, which the wave turns over in LDS of its own into the
 // fragments of v_mfma_f32_16x16x32 (loading those straight from memory, 64 bytes of
-// sixteen rows at a time, took 78 us for 16 tokens, 4096 x 11264; 56 this way).  The
-// next piece is in flight meanwhile.  The waves' sums meet in LDS, in wave order.
-// Eight waves per workgroup (69 us) and 32 rows of B (61 us) keep fewer pieces in
-// flight.  One token, 4096 x 11264: 34 us for the first product's 184 MB, 18 for the
-// second's 92, each with about 3 us of launch and first loads.
+// sixteen rows at a time, took 78 us for 16 tokens, 4096 x 11264; 56 this way, 61 where
+// every call has other weights).  The next piece is in flight meanwhile.  The waves'
+// sums meet in LDS, in wave order.  Eight waves per workgroup (69 us, the same weights)
+// and 32 rows of B (61 us) keep fewer pieces in flight.  One token, 4096 x 11264: 34 us for the first product's 184 MB, 18 for the
+// second's 92, each with about 3 us of launch and first loads.  Every workgroup reads
+// all of A from L2: at 16 tokens, 4096 wide, as many bytes as its weights (37 + 20 us).
 #include <algorithm>
 
 #include "common.hpp"

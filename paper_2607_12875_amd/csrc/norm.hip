@@ -5,10 +5,11 @@
 //   g = dy w;  dx = rstd (g - mean(g) - xhat mean(g xhat)) + dsum  (rms: no mean(g))
 //   dw = sum over rows of dy xhat;  db = sum over rows of dy
 // All of it is bound by HBM, so a row is read once and held in registers: a row
-// group of G threads, each with NV chunks of 16 bytes.  The variance is summed
-// about the mean, in a second pass over the registers.  A width that no chunk
-// divides leaves rows off their 16-byte alignment, which the memory takes, and a
-// last chunk that is read element by element.
+// group of G threads, whole waves, each with NV chunks of 16 bytes.  Narrow rows leave
+// lanes of their wave idle: 262144 x 128 bf16, 16 of 64, runs at 2.0 TB/s forward.
+// The variance is summed about the mean, in a second pass over the registers.  A
+// width that no chunk divides leaves rows off their 16-byte alignment, which the
+// memory takes, and a last chunk that is read element by element.
 #include <algorithm>
 #include <type_traits>
 
@@ -187,7 +188,12 @@ __device__ __forceinline__ void put4(float* row, int h, int end, const f32x4& v)
 // the barrier of every row stood between the loads (8192 x 4096 bf16 with dsum, 268
 // MB: 102 us; 46 now).  Rows so wide that a thread has several chunks keep
 // the column sums in LDS (IN_LDS; each thread its own columns, so without atomics),
-// where they fit: in registers they would spill.
+// where they fit, to 20224 elements.  With two chunks all else stays in registers
+// (2048 x 16384 bf16, 201 MB: 44 us).  With more, 16-bit rows past 16384 elements and
+// fp32 rows past 8192, the 128 registers of 1024 threads do not hold the row, the
+// next one and the weight, nor the sums past LDS: four fp32 chunks spill 110 bytes a
+// lane (4096 x 16384, 805 MB: 184 us), four 16-bit ones 0.5 to 0.7 KB (4096 x 18432 bf16, 453
+// MB: 300 us), eight 0.7 to 1.8 KB (1024 x 40008 bf16, 246 MB: 735 us), sixteen 2 KB.
 template <class E, int NV, int KIND, bool IN_LDS>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackward a, int G) {
   using C = Chunk<E>;
