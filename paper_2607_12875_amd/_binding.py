@@ -315,10 +315,8 @@ def moe_forward(hidden, logits, w1, w2, top_k, *, mode="softmax", renormalize=Tr
 
 
 # ------------------------------------------------- norm, feed-forward block
-# These calls and their backward passes are apart: results carry no autograd graph,
-# whether or not the inputs require gradients.  As under torch.cuda.stream, a caller
-# who frees inputs that another stream allocated before stream= has run the call
-# tells the allocator (Tensor.record_stream).
+# As under torch.cuda.stream, a caller who frees inputs that another stream allocated
+# before stream= has run the call tells the allocator (Tensor.record_stream).
 def _sizes(where, *n):
     """Refuse a size that a C int would cut, as the library refuses one past its limits."""
     if min(n) < -1 << 31 or max(n) >= 1 << 31:
@@ -388,7 +386,8 @@ def moe_norm_forward(x, weight, *, bias=None, residual=None, kind="layer", eps=1
 
     s is what was normalised: x itself, or the sum rounded to the type (in
     sum_out where given).  mean and rstd (fp32 [T], for moe_norm_backward) are
-    None without stats, mean also for "rms".  weight and bias [H] in x's type."""
+    None without stats, mean also for "rms".  weight and bias [H] in x's type.
+    Results carry no autograd graph: moe_norm_backward is a call of its own."""
     shape, i = _rows(x, "x")
     T, H = shape
     dt, dtype = x.dtype, _dtype(x, "x")
@@ -477,7 +476,8 @@ def moe_ffn_forward(x, w1, w2, *, act="silu", add=None, save=False, y=None, pre=
     With save, or into a pre that is given, pre (fp32 [T,2I]) keeps both
     projections for moe_ffn_backward, else it is None.  add [T,H] may be y itself.
     workspace: a uint8 tensor, kept from call to call; without, or with fewer than
-    moe_ffn_workspace_bytes, a new one, which is returned."""
+    moe_ffn_workspace_bytes, a new one, which is returned.  Results carry no
+    autograd graph: moe_ffn_backward is a call of its own."""
     shape, i = _rows(x, "x")
     T, H = shape
     I, dt = w2.shape[-1], x.dtype

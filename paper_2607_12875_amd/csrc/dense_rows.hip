@@ -8,9 +8,10 @@
 // sixteen rows at a time, took 78 us for 16 tokens, 4096 x 11264; 56 this way, 61 where
 // every call has other weights).  The next piece is in flight meanwhile.  The waves'
 // sums meet in LDS, in wave order.  Eight waves per workgroup (69 us, the same weights)
-// and 32 rows of B (61 us) keep fewer pieces in flight.  One token, 4096 x 11264: 34 us for the first product's 184 MB, 18 for the
-// second's 92, each with about 3 us of launch and first loads.  Every workgroup reads
-// all of A from L2: at 16 tokens, 4096 wide, as many bytes as its weights (37 + 20 us).
+// and 32 rows of B (61 us) keep fewer pieces in flight.  One token, 4096 x 11264: 34
+// us for the first product's 184 MB, 18 for the second's 92, each with about 3 us of
+// launch and first loads.  Every workgroup reads all of A from L2: at 16 tokens, 4096
+// wide, as many bytes as its weights (37 + 20 us).
 #include <algorithm>
 
 #include "common.hpp"
